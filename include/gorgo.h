@@ -479,6 +479,96 @@ int gorgo_eval_population_static(gorgo_sim_t *sim, uint32_t n_candidates, const 
 
 const char *gorgo_strerror(int code);
 
+/* ------------------------------------------------------------------ paged key-value cache
+ * The service model above takes an engine's times as constants; the entry points below are the part of
+ * such an engine that its cache decides: keys and values of prompts in blocks of tokens ("pages"), and
+ * the attention over them.  What gorgo_route_batch calls a prefix hit is that the leading pages of a
+ * prompt are there: gorgo_attn_prefill computes the uncached rest on top of them (the paper's
+ * prefill(x_r \ c_i), Eq. 1), gorgo_attn_decode one more token of every running request.
+ *
+ * Pool: k and v are [n_pages][n_kv_heads][page_tokens][head_dim]; token j of sequence s lies in page
+ * table[s * table_stride + j / page_tokens], slot j % page_tokens.  Types: bf16 or fp16 as they are, or
+ * e4m3 codes with one power of two 2^e per token and head (e is the least integer >= -24 with
+ * max|x| <= 448 * 2^e; a code is x * 2^-e rounded to nearest even; it stands for code * 2^e).  A row that
+ * holds a NaN or an infinity is stored in e4m3 as NaN throughout.
+ *
+ * The calls only enqueue kernels on `cuda_stream` (they may be captured into a graph) and keep nothing
+ * between them.  All arrays are DEVICE memory of `device`.  The lengths and the table are read on the device: the
+ * kernels check them, never leave the given arrays, and report what is wrong in `status` (bits
+ * GORGO_KV_*, set and never cleared); outputs of a sequence with a wrong page or length hold NaN (attention, read) or its
+ * wrong tokens are left out (write).  A page that is written must not be in the table twice in one batch. */
+enum { GORGO_BF16 = 0, GORGO_FP16 = 1, GORGO_E4M3 = 2 };
+enum {
+  GORGO_KV_BAD_PAGE = 1,              /* a table entry that is needed is outside [0, n_pages)       */
+  GORGO_KV_BAD_LENGTH = 2,            /* cu_new or kv_len decreasing, negative or above its bound   */
+  GORGO_KV_WAIT_LIMIT = 4             /* a bounded wait inside a kernel ran out                     */
+};
+
+typedef struct gorgo_kv_cache {
+  void *k, *v;                  /* DEVICE pools, 128-byte aligned                                   */
+  int8_t *k_exp, *v_exp;        /* DEVICE [n_pages][n_kv_heads][page_tokens], 16-byte aligned, for  */
+                                /* GORGO_E4M3; NULL for the other types                            */
+  uint32_t n_pages;             /* >= 1; n_pages * n_kv_heads * page_tokens < 2^31                 */
+  uint32_t page_tokens;         /* a power of two, 16..1024                                        */
+  uint32_t n_kv_heads;          /* 1..1024                                                         */
+  uint32_t head_dim;            /* 64 or 128                                                       */
+  uint32_t type;                /* GORGO_BF16, GORGO_FP16 or GORGO_E4M3                            */
+  int32_t device;               /* CUDA device ordinal                                             */
+} gorgo_kv_cache_t;
+
+/* A batch of sequences: cu_new[s]..cu_new[s+1] are the rows of sequence s's new tokens in a packed
+ * array; they are its last tokens, kv_len[s] counts all of them.  The four numbers on the host bound what
+ * the device arrays say (a graph may be replayed with other lengths under the same bounds). */
+typedef struct gorgo_kv_batch {
+  uint32_t n_seqs;              /* 0..65535; 0: nothing is done                                     */
+  uint32_t total_new;           /* rows of the packed array, >= cu_new[n_seqs], < 2^24              */
+  uint32_t max_new;             /* most new tokens of one sequence                                 */
+  uint32_t max_kv;              /* most tokens of one sequence, < 2^24                             */
+  uint64_t total_kv;            /* bound of the sum of kv_len                                      */
+  uint32_t table_stride;        /* entries from one row of the table to the next; table_stride *   */
+                                /* page_tokens >= max_kv                                           */
+  uint32_t reserved;            /* must be 0                                                       */
+  const int32_t *cu_new;        /* DEVICE [n_seqs + 1]                                             */
+  const int32_t *kv_len;        /* DEVICE [n_seqs]                                                 */
+  const int32_t *table;         /* DEVICE [n_seqs][table_stride]; entries not needed may hold anything */
+  uint32_t *status;             /* DEVICE, one word, or NULL                                       */
+} gorgo_kv_batch_t;
+
+/* New tokens into their pages.  k_new, v_new: DEVICE rows of `type` (bf16 or fp16; the cache's own type
+ * unless that is e4m3), token t at t * stride elements, its heads one after the other; 16-byte aligned,
+ * strides multiples of 8.  Slots behind a sequence's last token are left as they are. */
+int gorgo_kv_write(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch, const void *k_new,
+                   const void *v_new, uint32_t type, uint64_t k_stride, uint64_t v_stride,
+                   void *cuda_stream);
+
+/* The same tokens out of their pages, in `type` (bf16 or fp16; the cache's own unless that is e4m3).
+ * Rows behind cu_new[n_seqs] are left as they are. */
+int gorgo_kv_read(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch, void *k_out,
+                  void *v_out, uint32_t type, uint64_t k_stride, uint64_t v_stride,
+                  void *cuda_stream);
+
+/* Attention of queries against the pages.  q, out: DEVICE rows of `type` (bf16 or fp16; the cache's own
+ * unless that is e4m3), n_heads a multiple of n_kv_heads (at most 128 times as many), query head h reads kv head
+ * h / (n_heads / n_kv_heads); row strides in elements, multiples of 8, 16-byte aligned.  With z_j = scale * (q . k_j)
+ * over the keys j that a row sees: out = sum_j exp(z_j) v_j / sum_j exp(z_j), lse (DEVICE
+ * float [rows][n_heads], or NULL) = log sum_j exp(z_j).  A row that sees no key gets zeros and -inf.
+ *   gorgo_attn_prefill: one row per new token; the token at position p of its sequence sees the keys 0..p
+ * (those of the new tokens are written first).  Rows behind cu_new[n_seqs] are left as they are.
+ *   gorgo_attn_decode: one row per sequence, which sees all its kv_len[s] keys; cu_new, total_new and
+ * max_new are not used.
+ * `workspace`: DEVICE, 256-byte aligned, of at least the bytes that gorgo_attn_workspace_bytes says for the
+ * same arguments; nothing in it is kept, and calls that may run at the same time need one each. */
+int gorgo_attn_workspace_bytes(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch,
+                               uint32_t n_heads, uint32_t type, int decode, uint64_t *bytes_out);
+int gorgo_attn_prefill(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch, const void *q,
+                       uint32_t n_heads, uint32_t type, uint64_t q_stride, double scale, void *out,
+                       uint64_t out_stride, float *lse, void *workspace, uint64_t workspace_bytes,
+                       void *cuda_stream);
+int gorgo_attn_decode(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch, const void *q,
+                      uint32_t n_heads, uint32_t type, uint64_t q_stride, double scale, void *out,
+                      uint64_t out_stride, float *lse, void *workspace, uint64_t workspace_bytes,
+                      void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,7 +37,11 @@ EXPORTS = [
     "gorgo_sim_set_replica_speeds", "gorgo_debug_set", "gorgo_measure_gather", "gorgo_tune_online",
     "gorgo_sim_set_service_model", "gorgo_sim_set_rtt_series", "gorgo_sim_set_proxy_index",
     "gorgo_trace_begin", "gorgo_trace_append",
+    "gorgo_kv_write", "gorgo_kv_read", "gorgo_attn_workspace_bytes", "gorgo_attn_prefill",
+    "gorgo_attn_decode",
 ]
+GORGO_BF16, GORGO_FP16, GORGO_E4M3 = 0, 1, 2
+GORGO_KV_BAD_PAGE, GORGO_KV_BAD_LENGTH, GORGO_KV_WAIT_LIMIT = 1, 2, 4
 GORGO_DEBUG_POLL_LIMIT, GORGO_DEBUG_RING_POLLS, GORGO_DEBUG_PROBE_OFF, GORGO_DEBUG_SCOUT_OFF = 0, 1, 2, 3
 GORGO_DEBUG_BUILD = 4
 
@@ -61,6 +65,19 @@ class gorgo_online_config_t(C.Structure):
     _fields_ = [("n_tuned", C.c_uint32), ("n_draw_steps", C.c_uint32), ("window", C.c_uint32),
                 ("hop", C.c_uint32), ("tuned", C.c_void_p), ("lo", C.c_void_p), ("hi", C.c_void_p),
                 ("sigma0", C.c_double), ("sigma_up", C.c_double), ("time_scale", C.c_double)]
+
+
+class gorgo_kv_cache_t(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("n_pages", C.c_uint32), ("page_tokens", C.c_uint32), ("n_kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("type", C.c_uint32), ("device", C.c_int32)]
+
+
+class gorgo_kv_batch_t(C.Structure):
+    _fields_ = [("n_seqs", C.c_uint32), ("total_new", C.c_uint32), ("max_new", C.c_uint32),
+                ("max_kv", C.c_uint32), ("total_kv", C.c_uint64), ("table_stride", C.c_uint32),
+                ("reserved", C.c_uint32), ("cu_new", C.c_void_p), ("kv_len", C.c_void_p),
+                ("table", C.c_void_p), ("status", C.c_void_p)]
 
 
 class GorgoError(RuntimeError):
@@ -119,6 +136,11 @@ def load():
         "gorgo_set_profiling": [vp, i32],
         "gorgo_last_replay_ms": [vp, C.POINTER(C.c_double), C.POINTER(C.c_uint32)],
         "gorgo_last_window_ms": [vp, C.POINTER(C.c_double), C.POINTER(C.c_uint32)],
+        "gorgo_kv_write": [vp, vp, vp, vp, u32, u64, u64, vp],
+        "gorgo_kv_read": [vp, vp, vp, vp, u32, u64, u64, vp],
+        "gorgo_attn_workspace_bytes": [vp, vp, u32, u32, i32, pu64],
+        "gorgo_attn_prefill": [vp, vp, vp, u32, u32, u64, dbl, vp, u64, vp, vp, u64, vp],
+        "gorgo_attn_decode": [vp, vp, vp, u32, u32, u64, dbl, vp, u64, vp, vp, u64, vp],
     }
     for name, argtypes in sig.items():
         fn = getattr(lib, name)
@@ -452,7 +474,195 @@ def gorgo_last_window_ms(sim):
     return rc, ms.value, n.value
 
 
-# ------------------------------------------------------------------------ buffer holder
+def _struct_ptr(x):
+    return None if x is None else C.addressof(x)
+
+
+def gorgo_kv_write(cache, batch, k_new, v_new, type, k_stride, v_stride, stream=0) -> int:
+    """``cache``: gorgo_kv_cache_t, ``batch``: gorgo_kv_batch_t; ``k_new``, ``v_new``: torch CUDA tensors."""
+    return load().gorgo_kv_write(_struct_ptr(cache), _struct_ptr(batch), _dev_ptr(k_new), _dev_ptr(v_new),
+                                 int(type), int(k_stride), int(v_stride), stream)
+
+
+def gorgo_kv_read(cache, batch, k_out, v_out, type, k_stride, v_stride, stream=0) -> int:
+    return load().gorgo_kv_read(_struct_ptr(cache), _struct_ptr(batch), _dev_ptr(k_out), _dev_ptr(v_out),
+                                int(type), int(k_stride), int(v_stride), stream)
+
+
+def gorgo_attn_workspace_bytes(cache, batch, n_heads, type, decode):
+    """Returns (status, bytes)."""
+    out = C.c_uint64()
+    rc = load().gorgo_attn_workspace_bytes(_struct_ptr(cache), _struct_ptr(batch), int(n_heads), int(type),
+                                           int(bool(decode)), C.byref(out))
+    return rc, out.value
+
+
+def gorgo_attn_prefill(cache, batch, q, n_heads, type, q_stride, scale, out, out_stride, lse, workspace,
+                       stream=0) -> int:
+    """``workspace``: torch CUDA uint8 tensor or None (where gorgo_attn_workspace_bytes says 0)."""
+    return load().gorgo_attn_prefill(_struct_ptr(cache), _struct_ptr(batch), _dev_ptr(q), int(n_heads), int(type),
+                                     int(q_stride), float(scale), _dev_ptr(out), int(out_stride), _dev_ptr(lse),
+                                     _dev_ptr(workspace), 0 if workspace is None else workspace.numel(), stream)
+
+
+def gorgo_attn_decode(cache, batch, q, n_heads, type, q_stride, scale, out, out_stride, lse, workspace,
+                      stream=0) -> int:
+    return load().gorgo_attn_decode(_struct_ptr(cache), _struct_ptr(batch), _dev_ptr(q), int(n_heads), int(type),
+                                    int(q_stride), float(scale), _dev_ptr(out), int(out_stride), _dev_ptr(lse),
+                                    _dev_ptr(workspace), 0 if workspace is None else workspace.numel(), stream)
+
+
+# ------------------------------------------------------------------------ buffer holders
+class GorgoKvBatch:
+    """Sequences of one call: their new tokens and their pages (plumbing only).
+
+    ``new`` and ``kv`` are the new tokens and the tokens in all of every sequence, on the host; ``table``
+    int32 [sequences, pages] on the GPU.  ``cu_new`` and ``kv_len`` are the same lengths on the GPU (made here
+    if not given); a captured graph may be replayed after they and the table were written anew, as long as the
+    lengths stay within the ones given here."""
+
+    def __init__(self, new, kv, table, *, cu_new=None, kv_len=None):
+        import torch
+        new, kv = [int(x) for x in new], [int(x) for x in kv]
+        if len(new) != len(kv) or min(new + kv, default=0) < 0:
+            raise ValueError("one number of new tokens and one of all tokens per sequence, none negative")
+        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != len(kv) or not table.is_cuda or \
+                (table.numel() and table.stride(1) != 1):
+            raise ValueError("table: int32 [sequences, pages] on the GPU, rows contiguous")
+        dev, n = table.device, len(kv)
+        if cu_new is None:
+            cu_new = torch.tensor(np.concatenate([[0], np.cumsum(new, dtype=np.int64)]), dtype=torch.int32, device=dev)
+        if kv_len is None:
+            kv_len = torch.tensor(kv, dtype=torch.int32, device=dev)
+        for x, m in ((cu_new, n + 1), (kv_len, n)):
+            if x.dtype != torch.int32 or x.shape != (m,) or not x.is_contiguous() or x.device != dev:
+                raise ValueError("cu_new [sequences + 1] and kv_len [sequences]: int32, contiguous, beside the table")
+        self.n_seqs, self.total_new, self.device = n, sum(new), dev
+        self.table, self.cu_new, self.kv_len = table, cu_new, kv_len
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.c = gorgo_kv_batch_t(n, self.total_new, max(new, default=0), max(kv, default=0), sum(kv),
+                                  table.stride(0) if n > 1 else table.shape[1], 0, cu_new.data_ptr(),
+                                  kv_len.data_ptr(), table.data_ptr(), self.status.data_ptr())
+        self.ptr = C.addressof(self.c)
+
+    def check(self):
+        """Waits for the GPU and raises if a kernel found a wrong page or length."""
+        bits = int(self.status.item())
+        if bits:
+            raise GorgoError(GORGO_ERR_DEVICE_LIMIT if bits & GORGO_KV_WAIT_LIMIT else GORGO_ERR_INVALID_ARG,
+                             f"key-value cache: status bits {bits}")
+
+
+class GorgoKvCache:
+    """Pools of pages as torch tensors and the calls on them, on the current stream (plumbing only).
+
+    ``k``, ``v``: [pages, kv heads, page tokens, head dim] in bfloat16, float16 or float8_e4m3fn; the last with
+    ``k_exp``, ``v_exp``: int8 [pages, kv heads, page tokens]."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        import torch
+        self._types = {torch.bfloat16: GORGO_BF16, torch.float16: GORGO_FP16}
+        types = {**self._types, torch.float8_e4m3fn: GORGO_E4M3}
+        if k.dtype not in types or k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not k.is_cuda or \
+                k.device != v.device or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("k and v: contiguous [pages, kv heads, page tokens, head dim] of one cache type on one GPU")
+        for e in (k_exp, v_exp):
+            if (e is None) != (k.dtype != torch.float8_e4m3fn) or \
+                    (e is not None and (e.dtype != torch.int8 or e.shape != k.shape[:3] or not e.is_contiguous()
+                                        or e.device != k.device)):
+                raise ValueError("k_exp and v_exp: contiguous int8 [pages, kv heads, page tokens] beside an e4m3 cache")
+        self.torch, self.k, self.v, self.k_exp, self.v_exp = torch, k, v, k_exp, v_exp
+        self.dtype, self.device = k.dtype, k.device
+        self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
+        self.c = gorgo_kv_cache_t(k.data_ptr(), v.data_ptr(), _dev_ptr(k_exp), _dev_ptr(v_exp), self.n_pages,
+                                  self.page_tokens, self.n_kv_heads, self.head_dim, types[k.dtype],
+                                  k.device.index)
+        self.ptr = C.addressof(self.c)
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, head_dim, dtype, page_tokens=512, device=0):
+        """A cache of ``n_pages`` pages, filled with zeros."""
+        import torch
+        dev = torch.device("cuda", device)
+        pools = [torch.zeros((n_pages, n_kv_heads, page_tokens, head_dim), dtype=dtype, device=dev) for _ in "kv"]
+        exps = [torch.zeros(pools[0].shape[:3], dtype=torch.int8, device=dev) for _ in "kv"] \
+            if dtype == torch.float8_e4m3fn else [None, None]
+        return cls(*pools, *exps)
+
+    def _rows(self, x, n, heads, what):
+        if x.dim() != 3 or x.shape[0] < n or x.shape[1] != heads or x.shape[2] != self.head_dim or \
+                x.device != self.device or x.stride(2) != 1 or x.stride(1) != self.head_dim or x.dtype not in self._types:
+            raise ValueError(f"{what}: [{n} rows or more, {heads} heads, {self.head_dim}] in 16 bits on the cache's GPU, "
+                             "the heads of a row one after the other")
+        return self._types[x.dtype]
+
+    def _stream(self):
+        return self.torch.cuda.current_stream(self.device).cuda_stream
+
+    def write(self, batch, k_new, v_new):
+        """Keys and values [new tokens, kv heads, head dim] of the batch's new tokens into their pages."""
+        t = self._rows(k_new, batch.total_new, self.n_kv_heads, "k_new")
+        if self._rows(v_new, batch.total_new, self.n_kv_heads, "v_new") != t:
+            raise ValueError("k_new and v_new: one type")
+        rc = load().gorgo_kv_write(self.ptr, batch.ptr, k_new.data_ptr(), v_new.data_ptr(), t, _row_stride(k_new),
+                                   _row_stride(v_new), self._stream())
+        if rc != GORGO_OK:
+            raise GorgoError(rc, "gorgo_kv_write")
+
+    def read(self, batch, dtype=None, out=None):
+        """Keys and values of the batch's new tokens as (k, v), each [new tokens, kv heads, head dim]."""
+        torch = self.torch
+        if out is None:
+            dtype = dtype or (self.dtype if self.dtype in self._types else torch.bfloat16)
+            shape = (batch.total_new, self.n_kv_heads, self.head_dim)
+            out = tuple(torch.empty(shape, dtype=dtype, device=self.device) for _ in "kv")
+        t = self._rows(out[0], batch.total_new, self.n_kv_heads, "out")
+        if self._rows(out[1], batch.total_new, self.n_kv_heads, "out") != t:
+            raise ValueError("out: one type")
+        rc = load().gorgo_kv_read(self.ptr, batch.ptr, out[0].data_ptr(), out[1].data_ptr(), t, _row_stride(out[0]),
+                                  _row_stride(out[1]), self._stream())
+        if rc != GORGO_OK:
+            raise GorgoError(rc, "gorgo_kv_read")
+        return out
+
+    def prefill(self, batch, q, scale=None, out=None, lse=None):
+        """Attention of the batch's new tokens, ``q`` [new tokens, heads, head dim], to everything before them
+        and themselves; their keys and values have been written.  ``lse``: float32 [rows, heads] or None."""
+        return self._attend(batch, q, scale, out, lse, batch.total_new, 0)
+
+    def decode(self, batch, q, scale=None, out=None, lse=None):
+        """Attention of one row per sequence, ``q`` [sequences, heads, head dim], to all its keys."""
+        return self._attend(batch, q, scale, out, lse, batch.n_seqs, 1)
+
+    def _attend(self, batch, q, scale, out, lse, rows, decode):
+        torch = self.torch
+        heads = q.shape[1] if q.dim() == 3 else 0
+        t = self._rows(q, rows, heads, "q")
+        if out is None:
+            out = torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=self.device)
+        elif self._rows(out, rows, heads, "out") != t:
+            raise ValueError("out: the type of q")
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.dim() != 2 or
+                                lse.shape[0] < rows or lse.shape[1] != heads or lse.device != self.device):
+            raise ValueError("lse: contiguous float32 [rows, heads] on the cache's GPU")
+        lib, need = load(), C.c_uint64()
+        name = "gorgo_attn_decode" if decode else "gorgo_attn_prefill"
+        rc = lib.gorgo_attn_workspace_bytes(self.ptr, batch.ptr, heads, t, decode, C.byref(need))
+        if rc != GORGO_OK:
+            raise GorgoError(rc, name)
+        ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+        rc = getattr(lib, name)(self.ptr, batch.ptr, q.data_ptr(), heads, t, _row_stride(q),
+                                self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), _row_stride(out),
+                                _dev_ptr(lse), _dev_ptr(ws), need.value, self._stream())
+        if rc != GORGO_OK:
+            raise GorgoError(rc, name)
+        return out
+
+
+def _row_stride(x):
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
 class GorgoSim:
     """Owns the handle and the torch tensors used as device buffers (plumbing only)."""
 

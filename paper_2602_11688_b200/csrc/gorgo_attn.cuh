@@ -1,0 +1,142 @@
+// What the kernels of the paged key-value cache share: views of the cache and of a batch, where a token
+// lies, and the two 16-bit types.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/gorgo.h"
+
+namespace gorgo {
+
+constexpr int kExpMin = -24;              // least exponent of a quantised row
+
+struct KvView {
+  void* k;
+  void* v;
+  int8_t* k_exp;                          // null unless quantised
+  int8_t* v_exp;
+  uint32_t n_pages, page_shift, n_kv_heads;
+};
+
+struct BatchView {
+  const int32_t* cu_new;
+  const int32_t* kv_len;
+  const int32_t* table;
+  uint32_t* status;
+  uint32_t n_seqs, total_new, max_kv, table_stride;
+};
+
+// Launchers; every size has been checked by the caller.
+struct KvMoveArgs {
+  KvView kv;
+  BatchView b;
+  const void* k_in;                       // write: rows of new tokens
+  const void* v_in;
+  void* k_out;                            // read
+  void* v_out;
+  uint64_t k_stride, v_stride;            // elements from token to token
+  uint32_t head_dim, type, store;
+};
+cudaError_t launch_kv_write(const KvMoveArgs& a, cudaStream_t st);
+cudaError_t launch_kv_read(const KvMoveArgs& a, cudaStream_t st);
+
+struct AttnArgs {
+  KvView kv;
+  BatchView b;
+  const void* q;
+  void* out;
+  float* lse;                             // or null
+  uint64_t q_stride, out_stride;          // elements from row to row
+  uint32_t n_heads, group;                // group: query heads of a kv head
+  uint32_t head_dim, type, store;
+  float scale_log2;                       // scale * log2(e)
+  uint32_t max_new;
+  uint64_t total_kv;
+  void* workspace;
+};
+uint64_t attn_workspace(const AttnArgs& a, bool decode, int sms);
+cudaError_t launch_attn_prefill(const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attn_decode(const AttnArgs& a, int sms, cudaStream_t st);
+
+#ifdef __CUDACC__
+
+__device__ __forceinline__ void report(uint32_t* status, uint32_t bits) {
+  if (status) atomicOr(status, bits);
+}
+
+// 2^e for -126 <= e <= 127, exactly.
+__device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }
+
+template <typename T> struct Half2Of;
+template <> struct Half2Of<__nv_bfloat16> { using type = __nv_bfloat162; };
+template <> struct Half2Of<__half> { using type = __half2; };
+
+__device__ __forceinline__ float2 unpack2(uint32_t x, __nv_bfloat16) {
+  return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack2(uint32_t x, __half) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&x));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Two e4m3 codes (low byte first) as floats, exactly.
+__device__ __forceinline__ float2 unpack_e4m3(uint32_t two) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+  return __half22float2(__half2(h));
+}
+
+// New tokens and all tokens of sequence s; a wrong length is reported and counts as no tokens.
+struct SeqLen {
+  int first, n, kv;                       // first row, new tokens, tokens in all
+  bool ok;
+};
+__device__ __forceinline__ bool kv_len_ok(const BatchView& b, int kv) { return kv >= 0 && (uint32_t)kv <= b.max_kv; }
+__device__ __forceinline__ SeqLen seq_len(const BatchView& b, uint32_t s) {
+  const int a = b.cu_new[s], e = b.cu_new[s + 1], kv = b.kv_len[s];
+  SeqLen r = {a, e - a, kv, true};
+  if (a < 0 || e < a || (uint32_t)e > b.total_new || !kv_len_ok(b, kv)) {
+    report(b.status, GORGO_KV_BAD_LENGTH);
+    r.ok = false;
+  }
+  return r;
+}
+
+// Row of the pool (in units of head_dim elements) of token `j` of sequence s in kv head h; -1 if its page is
+// none.  Needs j < table_stride << page_shift.
+__device__ __forceinline__ int64_t pool_row(const KvView& kv, const BatchView& b, uint32_t s, uint32_t h, uint32_t j) {
+  const uint32_t page = (uint32_t)b.table[(size_t)s * b.table_stride + (j >> kv.page_shift)];
+  if (page >= kv.n_pages) return -1;
+  return (((int64_t)page * kv.n_kv_heads + h) << kv.page_shift) + (j & ((1u << kv.page_shift) - 1));
+}
+
+// Sequence whose rows hold row t, by a warp: the number of cu_new[1..n] that are <= t.  n_seqs if none holds it.
+__device__ __forceinline__ uint32_t warp_find_seq(const BatchView& b, uint32_t t, uint32_t lane) {
+  // 32 places at a time narrow the range (cu_new does not decrease; where it does, what is found is checked)
+  uint32_t lo = 0, hi = b.n_seqs;                          // the count lies in [lo, hi]
+  while (lo < hi) {
+    const uint32_t step = (hi - lo + 31) / 32;
+    const uint32_t at = lo + (lane + 1) * step;            // cu_new[at] <= t: at least `at` sequences end before t
+    const bool le = at <= hi && b.cu_new[at] <= (int)t;
+    const uint32_t c = __popc(__ballot_sync(0xffffffffu, le));
+    const uint32_t nlo = lo + c * step;
+    hi = min(hi, nlo + step - 1);
+    lo = min(nlo, hi);
+  }
+  return lo;
+}
+
+#endif  // __CUDACC__
+
+}  // namespace gorgo

@@ -1,0 +1,162 @@
+// C ABI of the paged key-value cache and its attention: argument checks and launches.  Nothing here allocates,
+// waits or keeps anything between calls.
+#include <cmath>
+
+#include "gorgo_attn.cuh"
+
+using namespace gorgo;
+
+namespace {
+
+// The device of the call for its duration.
+struct DeviceScope {
+  int prev = -1;
+  bool ok = true;
+  explicit DeviceScope(int dev) {
+    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; prev = -1; return; }
+    if (prev == dev) prev = -1;
+    else if (cudaSetDevice(dev) != cudaSuccess) ok = false;
+  }
+  ~DeviceScope() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+bool pow2(uint64_t x) { return x && (x & (x - 1)) == 0; }
+
+bool cache_ok(const gorgo_kv_cache_t* c) {
+  if (!c || !c->k || !c->v || !aligned(c->k, 128) || !aligned(c->v, 128)) return false;
+  if (c->type > GORGO_E4M3 || (c->head_dim != 64 && c->head_dim != 128) || c->device < 0) return false;
+  if (!pow2(c->page_tokens) || c->page_tokens < 16 || c->page_tokens > 1024) return false;
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_pages < 1) return false;
+  if ((uint64_t)c->n_pages * c->n_kv_heads * c->page_tokens >= (1ull << 31)) return false;   // rows: coordinates of a bulk copy
+  const bool exps = c->k_exp && c->v_exp && aligned(c->k_exp, 16) && aligned(c->v_exp, 16);
+  return c->type == GORGO_E4M3 ? exps : !c->k_exp && !c->v_exp;
+}
+
+bool batch_ok(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, bool decode) {
+  if (!b || b->reserved || b->n_seqs > 65535) return false;
+  if (b->n_seqs == 0) return true;
+  if (!b->kv_len || !b->table || (!decode && !b->cu_new)) return false;
+  if (!decode && (b->total_new >= (1u << 24) || b->max_new > b->total_new)) return false;
+  return b->max_kv < (1u << 24) && (uint64_t)b->table_stride * c->page_tokens >= b->max_kv;
+}
+
+bool type_ok(const gorgo_kv_cache_t* c, uint32_t type) {
+  return type <= GORGO_FP16 && (c->type == GORGO_E4M3 || c->type == type);
+}
+
+bool rows_ok(const void* p, uint64_t stride, uint64_t width) {
+  return p && aligned(p, 16) && stride % 8 == 0 && stride >= width && stride < (1ull << 32);
+}
+
+KvView view(const gorgo_kv_cache_t* c) {
+  return {c->k, c->v, c->k_exp, c->v_exp, c->n_pages, (uint32_t)__builtin_ctz(c->page_tokens), c->n_kv_heads};
+}
+BatchView view(const gorgo_kv_batch_t* b) {
+  return {b->cu_new, b->kv_len, b->table, b->status, b->n_seqs, b->total_new, b->max_kv, b->table_stride};
+}
+
+int move(bool write, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, const void* k, const void* v, uint32_t type,
+         uint64_t ks, uint64_t vs, void* stream) {
+  if (!cache_ok(c) || !batch_ok(c, b, false) || !type_ok(c, type)) return GORGO_ERR_INVALID_ARG;
+  if (b->n_seqs == 0 || b->total_new == 0) return GORGO_OK;
+  const uint64_t width = (uint64_t)c->n_kv_heads * c->head_dim;
+  if (!rows_ok(k, ks, width) || !rows_ok(v, vs, width)) return GORGO_ERR_INVALID_ARG;
+  DeviceScope dev(c->device);
+  if (!dev.ok) return GORGO_ERR_CUDA;
+  KvMoveArgs a = {view(c), view(b), k, v, const_cast<void*>(k), const_cast<void*>(v), ks, vs, c->head_dim, type, c->type};
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return (write ? launch_kv_write(a, st) : launch_kv_read(a, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
+}
+
+bool heads_ok(const gorgo_kv_cache_t* c, uint32_t n_heads) {
+  return n_heads && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= 128;
+}
+
+int sm_count(int device) {
+  int n = 0;
+  return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) == cudaSuccess ? n : 0;
+}
+
+AttnArgs attn_args(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, uint32_t n_heads, uint32_t type) {
+  AttnArgs a = {};
+  a.kv = view(c);
+  a.b = view(b);
+  a.n_heads = n_heads;
+  a.group = n_heads / c->n_kv_heads;
+  a.head_dim = c->head_dim;
+  a.type = type;
+  a.store = c->type;
+  a.max_new = b->max_new;
+  a.total_kv = b->total_kv;
+  return a;
+}
+
+int attend(bool decode, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, const void* q, uint32_t n_heads, uint32_t type,
+           uint64_t qs, double scale, void* out, uint64_t os, float* lse, void* ws, uint64_t ws_bytes, void* stream) {
+  if (!cache_ok(c) || !batch_ok(c, b, decode) || !type_ok(c, type) || !heads_ok(c, n_heads)) return GORGO_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return GORGO_ERR_NONFINITE_PARAM;
+  const uint64_t rows = b->n_seqs == 0 ? 0 : decode ? b->n_seqs : b->total_new;
+  if (rows == 0) return GORGO_OK;
+  const uint64_t width = (uint64_t)n_heads * c->head_dim;
+  if (rows * n_heads >= (1ull << 31) || !rows_ok(q, qs, width) || !rows_ok(out, os, width)) return GORGO_ERR_INVALID_ARG;
+  DeviceScope dev(c->device);
+  const int sms = dev.ok ? sm_count(c->device) : 0;
+  if (!sms) return GORGO_ERR_CUDA;
+  AttnArgs a = attn_args(c, b, n_heads, type);
+  const uint64_t need = attn_workspace(a, decode, sms);
+  if (need && (!ws || !aligned(ws, 256))) return GORGO_ERR_INVALID_ARG;
+  if (ws_bytes < need) return GORGO_ERR_WORKSPACE_TOO_SMALL;
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.q_stride = qs;
+  a.out_stride = os;
+  a.scale_log2 = (float)(scale * 1.4426950408889634074);
+  a.workspace = ws;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return (decode ? launch_attn_decode(a, sms, st) : launch_attn_prefill(a, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gorgo_kv_write(const gorgo_kv_cache_t* cache, const gorgo_kv_batch_t* batch, const void* k_new, const void* v_new,
+                   uint32_t type, uint64_t k_stride, uint64_t v_stride, void* cuda_stream) {
+  return move(true, cache, batch, k_new, v_new, type, k_stride, v_stride, cuda_stream);
+}
+
+int gorgo_kv_read(const gorgo_kv_cache_t* cache, const gorgo_kv_batch_t* batch, void* k_out, void* v_out, uint32_t type,
+                  uint64_t k_stride, uint64_t v_stride, void* cuda_stream) {
+  return move(false, cache, batch, k_out, v_out, type, k_stride, v_stride, cuda_stream);
+}
+
+int gorgo_attn_workspace_bytes(const gorgo_kv_cache_t* cache, const gorgo_kv_batch_t* batch, uint32_t n_heads, uint32_t type,
+                               int decode, uint64_t* bytes_out) {
+  if (!bytes_out || !cache_ok(cache) || !batch_ok(cache, batch, decode != 0) || !type_ok(cache, type) ||
+      !heads_ok(cache, n_heads))
+    return GORGO_ERR_INVALID_ARG;
+  *bytes_out = 0;
+  if (batch->n_seqs == 0) return GORGO_OK;
+  const int sms = sm_count(cache->device);
+  if (!sms) return GORGO_ERR_CUDA;
+  *bytes_out = attn_workspace(attn_args(cache, batch, n_heads, type), decode != 0, sms);
+  return GORGO_OK;
+}
+
+int gorgo_attn_prefill(const gorgo_kv_cache_t* cache, const gorgo_kv_batch_t* batch, const void* q, uint32_t n_heads,
+                       uint32_t type, uint64_t q_stride, double scale, void* out, uint64_t out_stride, float* lse,
+                       void* workspace, uint64_t workspace_bytes, void* cuda_stream) {
+  return attend(false, cache, batch, q, n_heads, type, q_stride, scale, out, out_stride, lse, workspace, workspace_bytes,
+                cuda_stream);
+}
+
+int gorgo_attn_decode(const gorgo_kv_cache_t* cache, const gorgo_kv_batch_t* batch, const void* q, uint32_t n_heads,
+                      uint32_t type, uint64_t q_stride, double scale, void* out, uint64_t out_stride, float* lse,
+                      void* workspace, uint64_t workspace_bytes, void* cuda_stream) {
+  return attend(true, cache, batch, q, n_heads, type, q_stride, scale, out, out_stride, lse, workspace, workspace_bytes,
+                cuda_stream);
+}
+
+}  // extern "C"
