@@ -114,8 +114,7 @@ cudaError_t dispatch_rows(const AttnArgs& a, bool decode, cudaStream_t st) {
 
 }  // namespace
 
-uint64_t attn_workspace(const AttnArgs&, bool, int) { return 0; }
+uint64_t attn_workspace(const AttnArgs& a, bool decode, int sms) { return decode ? decode_workspace(a, sms) : 0; }
 cudaError_t launch_attn_prefill(const AttnArgs& a, cudaStream_t st) { return dispatch_rows(a, false, st); }
-cudaError_t launch_attn_decode(const AttnArgs& a, int, cudaStream_t st) { return dispatch_rows(a, true, st); }
 
 }  // namespace gorgo

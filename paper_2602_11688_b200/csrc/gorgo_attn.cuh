@@ -59,6 +59,7 @@ struct AttnArgs {
   uint64_t total_kv;
   void* workspace;
 };
+uint64_t decode_workspace(const AttnArgs& a, int sms);
 uint64_t attn_workspace(const AttnArgs& a, bool decode, int sms);
 cudaError_t launch_attn_prefill(const AttnArgs& a, cudaStream_t st);
 cudaError_t launch_attn_decode(const AttnArgs& a, int sms, cudaStream_t st);

@@ -2,9 +2,38 @@
 // waits or keeps anything between calls.
 #include <cmath>
 
-#include "gorgo_attn.cuh"
+#include "gorgo_tma.cuh"
 
 using namespace gorgo;
+
+namespace gorgo {
+
+bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t head_dim, uint32_t type, uint32_t box_rows) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      fn = nullptr;
+    return reinterpret_cast<Encode>(fn);
+  }();
+  if (!encode) return false;
+  const uint32_t size = type == GORGO_E4M3 ? 1 : 2;
+  const uint32_t cols = head_dim * size < 128 ? head_dim : 128 / size;     // elements of a plane's row
+  const cuuint64_t dims[3] = {cols, rows, head_dim / cols};
+  const cuuint64_t strides[2] = {(cuuint64_t)head_dim * size, (cuuint64_t)cols * size};
+  const cuuint32_t box[3] = {cols, box_rows, head_dim / cols}, step[3] = {1, 1, 1};
+  const CUtensorMapDataType t = type == GORGO_E4M3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                : type == GORGO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encode(map, t, 3, const_cast<void*>(pool), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace gorgo
 
 namespace {
 
