@@ -103,8 +103,12 @@ bool heads_ok(const gorgo_kv_cache_t* c, uint32_t n_heads) {
 }
 
 int sm_count(int device) {
-  int n = 0;
-  return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) == cudaSuccess ? n : 0;
+  static std::atomic<int> known[64];
+  int n = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+  if (n) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
+  if (device < 64) known[device].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 AttnArgs attn_args(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, uint32_t n_heads, uint32_t type) {

@@ -5,12 +5,13 @@
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  o = sum o_i 2^(m_i - m) / l.
 //
 // What bounds it: every key and value is read once and used for `group` heads only, so HBM.  The work, all
-// (sequence, kv head) pairs with their keys in tiles of 64, is laid out as one line and cut into as many equal pieces as
+// (sequence, kv head) pairs with their keys in tiles of four slices, is laid out as one line and cut into as many equal pieces as
 // blocks fit the GPU at once: no length and no batch leaves an SM idle, and at most two pieces of a block are
 // partial; a second, small kernel joins those (it starts early and waits for the first one's end).
 //
-// Each of a block's four warps takes 16 keys of every tile and is on its own: its own ring of bulk copies, its
-// own running maximum and sum; warps meet only at the end of a (sequence, head).  Keys are the rows of the
+// Each of a block's four warps takes a slice of every tile, 4 KB of keys as far as that is 32 at most, and is on
+// its own: its own ring of bulk copies, its own running maximum and sum; warps meet only at the end of a
+// (sequence, head).  Keys are the rows of the
 // matrix instructions (S^T = K q^T, O^T = V^T P^T, 16 x 8 x 16), so that up to eight query heads cost what one
 // does; P is transposed between the two products by matrix moves.  P enters as the sum of two 16-bit numbers, so
 // that it is not what limits the result; the tensor pipe is nearly idle here.
@@ -25,19 +26,20 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kSlice = 16;                // keys of a warp in a tile
-constexpr int kTile = kWarps * kSlice;
 constexpr float kOffset = 14.f;           // p = 2^(z - m + kOffset): fp16 keeps p down to 2^-38 of the largest
 
 template <bool kQuant, int D>
 struct Sizes {
   static constexpr int kRow = D * (kQuant ? 1 : 2);            // bytes of a row
-  static constexpr int kPart = kSlice * kRow;                  // K or V of a warp's slice
-  static constexpr int kStages = kPart == 4096 ? 3 : kPart == 2048 ? (D == 128 ? 5 : 6) : 8;
+  static constexpr int kSlice = kRow == 256 ? 16 : 32;         // keys of a warp in a tile
+  static constexpr int kBlocks = kSlice / 16;
+  static constexpr int kTile = kWarps * kSlice;
+  static constexpr int kPart = kSlice * kRow;                  // K or V of a slice
+  static constexpr int kStages = kPart == 4096 ? 3 : 6;
   static constexpr int kRing = kWarps * kStages * 2 * kPart;
-  static constexpr int kPad = D + 4;                           // floats of a head's row in the merge buffer
+  static constexpr int kPad = 64 + 4;                          // floats of a head's row in the merge buffer: 64 dims at a time
   static constexpr int kMerge = kWarps * 8 * kPad * 4;
-  static constexpr int kExps = kQuant ? kWarps * kStages * 32 : 0;
+  static constexpr int kExps = kQuant ? kWarps * kStages * 2 * kSlice : 0;
   static constexpr int kBytes = kRing + kMerge + kExps + kWarps * 8 * 2 * 4 + kWarps * kStages * (8 + 4);
 };
 
@@ -47,8 +49,10 @@ struct Split {
   float* part_o;                          // [2 * grid][8 * NB][D]
   float* part_ml;                         // [2 * grid][8 * NB][2]
   uint32_t grid;                          // blocks of the first kernel
+  uint32_t box;                           // keys of one bulk copy: a slice, or a page where that is less
 };
 
+template <int kTile>
 __device__ __forceinline__ uint32_t tiles_of(const BatchView& b, uint32_t s) {
   const int kv = b.kv_len[s];
   return kv_len_ok(b, kv) ? (uint32_t)(kv + kTile - 1) / kTile : 0;
@@ -59,6 +63,7 @@ __device__ __forceinline__ uint32_t pieces(uint64_t total, uint32_t grid) {
   return total / 2 >= grid ? grid : total < 4 ? 1 : (uint32_t)(total / 2);
 }
 
+template <int kTile>
 struct Iter {                             // a place on the line of tiles
   uint32_t s, hh, tile, nt;
   int kv;
@@ -69,7 +74,7 @@ struct Iter {                             // a place on the line of tiles
     tile = 0;
     if (++hh < n_hh) return;
     hh = 0;
-    do { ++s; nt = tiles_of(b, s); } while (nt == 0);
+    do { ++s; nt = tiles_of<kTile>(b, s); } while (nt == 0);
     kv = b.kv_len[s];
   }
 };
@@ -106,7 +111,7 @@ __device__ __forceinline__ uint32_t codes_to_half2(uint16_t two) {
 template <bool kQuant, int D>
 __device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) {
   if (kQuant && D == 64) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
-  return (c >> 3) * (kSlice * 128) + r * 128 + (((c ^ r) & 7) << 4);
+  return (c >> 3) * (16 * 128) + r * 128 + (((c ^ r) & 7) << 4);
 }
 
 template <typename T, bool kQuant, int D, int NB>
@@ -114,12 +119,13 @@ __global__ void __launch_bounds__(kThreads, 2)
 decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using Z = Sizes<kQuant, D>;
   using M = typename std::conditional<kQuant, __half, T>::type;   // type of the matrix instructions' operands
-  constexpr int kSteps = D / 16, kH = 8 * NB;
+  constexpr int kSteps = D / 16, kH = 8 * NB, kSlice = Z::kSlice, kBlocks = Z::kBlocks;
+  constexpr bool kLow = !(kQuant && std::is_same<T, __nv_bfloat16>::value);   // fp16 P is exact enough for a bf16 result
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   unsigned char* ring = smem + warp * Z::kStages * 2 * Z::kPart;
   float* merge = reinterpret_cast<float*>(smem + Z::kRing);
-  unsigned char* exps = smem + Z::kRing + Z::kMerge + warp * Z::kStages * 32;
+  unsigned char* exps = smem + Z::kRing + Z::kMerge + warp * Z::kStages * 2 * kSlice;
   float* ml = reinterpret_cast<float*>(smem + Z::kRing + Z::kMerge + Z::kExps);        // [warp][8][2]
   uint64_t* bars = reinterpret_cast<uint64_t*>(ml + kWarps * 8 * 2);
   uint32_t* bad_page = reinterpret_cast<uint32_t*>(bars + kWarps * Z::kStages) + warp * Z::kStages;
@@ -134,11 +140,11 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
   launch_dependents();
 
   // this block's piece of the line, found by every warp for itself
-  Iter use;
+  Iter<Z::kTile> use;
   uint64_t seg_first;                     // first tile of sequence use.s on the line
   {
     uint64_t total = 0;
-    for (uint32_t s = lane; s < a.b.n_seqs; s += 32) total += tiles_of(a.b, s);
+    for (uint32_t s = lane; s < a.b.n_seqs; s += 32) total += tiles_of<Z::kTile>(a.b, s);
 #pragma unroll
     for (int d = 16; d; d /= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
     total *= sp.hh;
@@ -148,7 +154,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
     uint64_t before = 0;
     uint32_t s0 = 0, mine = 0, here = 0;
     for (;; s0 += 32) {                   // the sequence that holds tile `lo`
-      mine = s0 + lane < a.b.n_seqs ? tiles_of(a.b, s0 + lane) : 0;
+      mine = s0 + lane < a.b.n_seqs ? tiles_of<Z::kTile>(a.b, s0 + lane) : 0;
       uint64_t upto = mine;
 #pragma unroll
       for (int d = 1; d < 32; d *= 2) {
@@ -172,26 +178,32 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
     use.tile = (uint32_t)(off % use.nt);
     use.left = (uint32_t)(hi - lo);
   }
-  Iter get = use;
+  Iter<Z::kTile> get = use;
   __syncwarp();
 
   // Copies of a warp's slice of tile `get` into stage `st`.
   auto issue = [&](uint32_t st) {
     if (lane == 0) {
-      const uint32_t p0 = get.tile * kTile + warp * kSlice, bar = bar_a + 8 * st;
-      if ((int)p0 >= get.kv) {
+      const uint32_t p0 = get.tile * Z::kTile + warp * kSlice, bar = bar_a + 8 * st;
+      const int n = get.kv - (int)p0;     // keys from here on; only pieces that hold some have a page
+      if (n <= 0) {
         mbar_arrive(bar);
       } else {
-        int64_t row = pool_row(a.kv, a.b, get.s, get.hh / sp.ng, p0);
-        bad_page[st] = row < 0;
-        if (row < 0) { report(a.b.status, GORGO_KV_BAD_PAGE); row = 0; }   // (copies something that is there)
-        mbar_expect(bar, 2 * Z::kPart + (kQuant ? 32 : 0));
-        tma_rows(ring_a + st * 2 * Z::kPart, &k_map, (int)row, bar);
-        tma_rows(ring_a + st * 2 * Z::kPart + Z::kPart, &v_map, (int)row, bar);
-        if (kQuant) {
-          bulk_copy(exps_a + st * 32, a.kv.k_exp + row, 16, bar);
-          bulk_copy(exps_a + st * 32 + 16, a.kv.v_exp + row, 16, bar);
+        const uint32_t pieces = min((uint32_t)n + sp.box - 1, (uint32_t)kSlice) / sp.box;
+        mbar_expect(bar, pieces * sp.box * 2 * (Z::kRow + (kQuant ? 1 : 0)));
+        uint32_t wrong = 0;
+        for (uint32_t i = 0, r = 0; i < pieces; ++i, r += sp.box) {
+          int64_t row = pool_row(a.kv, a.b, get.s, get.hh / sp.ng, p0 + r);
+          if (row < 0) { report(a.b.status, GORGO_KV_BAD_PAGE); wrong = 1; row = 0; }   // (copies something that is there)
+          const uint32_t to = ring_a + st * 2 * Z::kPart + r * Z::kRow;
+          tma_rows(to, &k_map, (int)row, bar);
+          tma_rows(to + Z::kPart, &v_map, (int)row, bar);
+          if (kQuant) {
+            bulk_copy(exps_a + st * 2 * kSlice + r, a.kv.k_exp + row, sp.box, bar);
+            bulk_copy(exps_a + st * 2 * kSlice + kSlice + r, a.kv.v_exp + row, sp.box, bar);
+          }
         }
+        bad_page[st] = wrong;
       }
     }
     get.next(a.b, sp.hh);
@@ -256,7 +268,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
       fresh = false;
     }
 
-    const int p0 = (int)(use.tile * kTile + warp * kSlice), n_keys = use.kv - p0;
+    const int n_keys = use.kv - (int)(use.tile * Z::kTile + warp * kSlice);
     const uint32_t bar = bar_a + 8 * st;
     if (flying && !__all_sync(0xffffffffu, mbar_wait(bar, phase))) {
       alive = false;                      // no more copies; those that fly are waited for in their turn
@@ -265,70 +277,74 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
     if (n_keys > 0 && alive) {
       bad |= bad_page[st] != 0;
       const uint32_t ka = ring_a + st * 2 * Z::kPart, va = ka + Z::kPart;
-      float c[NB][4];
+      float c[kBlocks][NB][4];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[nb][i] = 0.f;
-      if (!kQuant) {
-        const uint32_t r = lane & 15, hi = lane >> 4;
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
+          for (int i = 0; i < 4; ++i) c[b][nb][i] = 0.f;
+        const uint32_t r = 16 * b + (lane & 15), hi = lane >> 4;
+#pragma unroll
+        for (int k = 0; k < kSteps; k += (kQuant ? 2 : 1)) {
           uint32_t f[4];
-          ldsm4(f, ka + chunk_at<kQuant, D>(r, 2 * k + hi));
+          if (!kQuant) {
+            ldsm4(f, ka + chunk_at<kQuant, D>(r, 2 * k + hi));
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) mma(c[nb], f, qf[nb][k][0], qf[nb][k][1], M());
-        }
-      } else {
-        const uint32_t r = lane & 15, hi = lane >> 4;
+            for (int nb = 0; nb < NB; ++nb) mma(c[b][nb], f, qf[nb][k][0], qf[nb][k][1], M());
+          } else {
+            ldsm4(f, ka + chunk_at<kQuant, D>(r, k + hi));     // two steps' codes: four neighbours of a row each
 #pragma unroll
-        for (int k = 0; k < kSteps; k += 2) {
-          uint32_t f[4];
-          ldsm4(f, ka + chunk_at<kQuant, D>(r, k + hi));       // two steps' codes: four neighbours of a row each
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t x[4] = {codes_to_half2((uint16_t)f[2 * i]), codes_to_half2((uint16_t)f[2 * i + 1]),
+                                     codes_to_half2((uint16_t)(f[2 * i] >> 16)), codes_to_half2((uint16_t)(f[2 * i + 1] >> 16))};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t x[4] = {codes_to_half2((uint16_t)f[2 * i]), codes_to_half2((uint16_t)f[2 * i + 1]),
-                                   codes_to_half2((uint16_t)(f[2 * i] >> 16)), codes_to_half2((uint16_t)(f[2 * i + 1] >> 16))};
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma(c[nb], x, qf[nb][k + i][0], qf[nb][k + i][1], M());
+              for (int nb = 0; nb < NB; ++nb) mma(c[b][nb], x, qf[nb][k + i][0], qf[nb][k + i][1], M());
+            }
           }
         }
       }
-      // rows g and g + 8 of S^T: this thread's two keys; columns 2t and 2t + 1: its two heads
-      float ks[2] = {1.f, 1.f}, ve[2] = {0.f, 0.f}, vi[2] = {1.f, 1.f};
-      if (kQuant) {
-        const int8_t* e = reinterpret_cast<const int8_t*>(exps + st * 32);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const bool have = (int)(g + 8 * i) < n_keys;         // (behind the last key lies anything)
-          ks[i] = pow2i(have ? e[g + 8 * i] : 0);
-          const int v = have ? e[16 + g + 8 * i] : 0;
-          ve[i] = (float)v;
-          vi[i] = pow2i(-v);              // l sums p without the values' powers of two
-        }
-      }
+      // rows g and g + 8 of a block of S^T: this thread's two keys; columns 2t and 2t + 1: its two heads
+      float vi[kBlocks][2];               // what l takes p times: the values' powers of two go into P alone
       const bool part = n_keys < kSlice;
       bool grow = false;
-      float top[NB][2];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float z = c[nb][i] * zs[nb][i & 1];
-          if (kQuant) z = __fmaf_rn(z, ks[i >> 1], ve[i >> 1]);
-          if (part && (int)(g + 8 * (i >> 1)) >= n_keys) z = -INFINITY;
-          c[nb][i] = z;
-        }
+      for (int b = 0; b < kBlocks; ++b) {
+        const int8_t* e = reinterpret_cast<const int8_t*>(exps + st * 2 * kSlice) + 16 * b + g;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float x = fmaxf(c[nb][i], c[nb][i + 2]);
+          const bool have = 16 * b + (int)g + 8 * i < n_keys;  // (behind the last key lies anything)
+          float ks = 1.f, ve = 0.f;
+          vi[b][i] = 1.f;
+          if (kQuant) {
+            ks = pow2i(have ? e[8 * i] : 0);
+            const int v = have ? e[kSlice + 8 * i] : 0;
+            ve = (float)v;
+            vi[b][i] = pow2i(-v);
+          }
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float z = c[b][nb][2 * i + j] * zs[nb][j];
+              if (kQuant) z = __fmaf_rn(z, ks, ve);
+              c[b][nb][2 * i + j] = part && !have ? -INFINITY : z;
+            }
+        }
+      }
+      float top[NB][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float x = fmaxf(c[0][nb][i], c[0][nb][i + 2]);
+          if (kBlocks == 2) x = fmaxf(x, fmaxf(c[kBlocks - 1][nb][i], c[kBlocks - 1][nb][i + 2]));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
           top[nb][i] = x;
           grow |= x > m[nb][i];
         }
-      }
       if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -346,52 +362,60 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
             for (int i = 0; i < 4; ++i) o[nb][k][i] *= f[i & 1];
         }
       }
-      uint32_t ph[NB][2], pl[NB][2];      // P as the second operand (k = key, n = head), high and low part
+      uint32_t ph[kBlocks][NB][2], pl[kBlocks][NB][2];   // P as the second operand (k = key, n = head), high and low part
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const float m0 = m[nb][0] == -INFINITY ? 0.f : m[nb][0] - kOffset, m1 = m[nb][1] == -INFINITY ? 0.f : m[nb][1] - kOffset;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {     // key g + 8 i
-          const float x = fast_exp2(c[nb][2 * i] - m0), y = fast_exp2(c[nb][2 * i + 1] - m1);
-          l[nb][0] = __fmaf_rn(x, vi[i], l[nb][0]);
-          l[nb][1] = __fmaf_rn(y, vi[i], l[nb][1]);
-          const uint32_t hi = pack2(x, y, M());
-          const float2 h = unpack2(hi, M());
-          ph[nb][i] = transpose8(hi);
-          pl[nb][i] = transpose8(pack2(x - h.x, y - h.y, M()));
-        }
-      }
-      // values behind the last key may be anything: they enter as zeros
-      const uint32_t keep0 = ((int)(2 * t) < n_keys ? 0xffffu : 0) | ((int)(2 * t + 1) < n_keys ? 0xffff0000u : 0);
-      const uint32_t keep8 = ((int)(2 * t + 8) < n_keys ? 0xffffu : 0) | ((int)(2 * t + 9) < n_keys ? 0xffff0000u : 0);
+        for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int k = 0; k < kSteps; k += (kQuant ? 2 : 1)) {
-        uint32_t f[4];
-        if (!kQuant) {
-          ldsm4t(f, va + chunk_at<kQuant, D>((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
-          if (part) { f[0] &= keep0; f[1] &= keep0; f[2] &= keep8; f[3] &= keep8; }
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            mma(o[nb][k], f, ph[nb][0], ph[nb][1], M());
-            mma(o[nb][k], f, pl[nb][0], pl[nb][1], M());
-          }
-        } else {
-          // two columns of 16 dims: a register holds dims 2g, 2g + 1 of keys 2t (low half) and 2t + 1
-          ldsm4t(f, va + chunk_at<kQuant, D>(lane & 15, k + (lane >> 4)));
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t x[4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const uint32_t lo = codes_to_half2((uint16_t)f[2 * i + j]), hi = codes_to_half2((uint16_t)(f[2 * i + j] >> 16));
-              x[2 * j] = __byte_perm(lo, hi, 0x5410);           // dim 2g of keys 2t, 2t + 1
-              x[2 * j + 1] = __byte_perm(lo, hi, 0x7632);       // dim 2g + 1
+          for (int i = 0; i < 2; ++i) {   // key g + 8 i
+            const float x = fast_exp2(c[b][nb][2 * i] - m0), y = fast_exp2(c[b][nb][2 * i + 1] - m1);
+            l[nb][0] = __fmaf_rn(x, vi[b][i], l[nb][0]);
+            l[nb][1] = __fmaf_rn(y, vi[b][i], l[nb][1]);
+            const uint32_t hi = pack2(x, y, M());
+            ph[b][nb][i] = transpose8(hi);
+            if (kLow) {
+              const float2 h = unpack2(hi, M());
+              pl[b][nb][i] = transpose8(pack2(x - h.x, y - h.y, M()));
             }
-            if (part) { x[0] &= keep0; x[1] &= keep0; x[2] &= keep8; x[3] &= keep8; }
+          }
+      }
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        // values behind the last key may be anything: they enter as zeros
+        const int n = n_keys - 16 * b;
+        const uint32_t keep0 = ((int)(2 * t) < n ? 0xffffu : 0) | ((int)(2 * t + 1) < n ? 0xffff0000u : 0);
+        const uint32_t keep8 = ((int)(2 * t + 8) < n ? 0xffffu : 0) | ((int)(2 * t + 9) < n ? 0xffff0000u : 0);
+#pragma unroll
+        for (int k = 0; k < kSteps; k += (kQuant ? 2 : 1)) {
+          uint32_t f[4];
+          if (!kQuant) {
+            ldsm4t(f, va + chunk_at<kQuant, D>(16 * b + (lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
+            if (part) { f[0] &= keep0; f[1] &= keep0; f[2] &= keep8; f[3] &= keep8; }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-              mma(o[nb][k + i], x, ph[nb][0], ph[nb][1], M());
-              mma(o[nb][k + i], x, pl[nb][0], pl[nb][1], M());
+              mma(o[nb][k], f, ph[b][nb][0], ph[b][nb][1], M());
+              if (kLow) mma(o[nb][k], f, pl[b][nb][0], pl[b][nb][1], M());
+            }
+          } else {
+            // two columns of 16 dims: a register holds dims 2g, 2g + 1 of key 2t (low half) and of key 2t + 1
+            ldsm4t(f, va + chunk_at<kQuant, D>(16 * b + (lane & 15), k + (lane >> 4)));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              uint32_t x[4];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const uint32_t y = __byte_perm(f[2 * i + j], 0, 0x3120);   // dim 2g of both keys, then dim 2g + 1
+                x[2 * j] = codes_to_half2((uint16_t)y);
+                x[2 * j + 1] = codes_to_half2((uint16_t)(y >> 16));
+              }
+              if (part) { x[0] &= keep0; x[1] &= keep0; x[2] &= keep8; x[3] &= keep8; }
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                mma(o[nb][k + i], x, ph[b][nb][0], ph[b][nb][1], M());
+                if (kLow) mma(o[nb][k + i], x, pl[b][nb][0], pl[b][nb][1], M());
+              }
             }
           }
         }
@@ -404,7 +428,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
     if (++st == (uint32_t)Z::kStages) { st = 0; phase ^= 1; }
 
     if (last || use.tile + 1 == use.nt) {
-      // the warps' sums of this (sequence, head) become one, eight heads at a time
+      // the warps' sums of this (sequence, head) become one, eight heads and 64 dims at a time
       const bool whole = first_tile == 0 && use.tile + 1 == use.nt;
       const uint32_t slot = 2 * blockIdx.x + (first_tile == 0 ? 1 : 0);
 #pragma unroll
@@ -424,42 +448,46 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
         }
         float* mo = merge + warp * 8 * Z::kPad;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k)
+        for (int part = 0; part < D / 64; ++part) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int dim = k * 16 + (kQuant ? 2 * g + (i >> 1) : g + 8 * (i >> 1));
-            mo[(2 * t + (i & 1)) * Z::kPad + dim] = o[nb][k][i];
-          }
-        __syncthreads();
-        for (uint32_t x = threadIdx.x; x < 8 * (D / 4); x += kThreads) {
-          const uint32_t h = x / (D / 4), d = x % (D / 4) * 4;
-          if (8 * nb + h >= n_h) continue;
-          float top = -INFINITY, sum = 0.f;
+          for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[(w * 8 + h) * 2]);
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = 0; i < 4; ++i) {
+              const int dim = k * 16 + (kQuant ? 2 * g + (i >> 1) : g + 8 * (i >> 1));
+              mo[(2 * t + (i & 1)) * Z::kPad + dim] = o[nb][4 * part + k][i];
+            }
+          __syncthreads();
+          static_assert(8 * 16 == kThreads, "a thread has four dims of a head");
+          const uint32_t h = threadIdx.x / 16, d = threadIdx.x % 16 * 4;
+          if (8 * nb + h < n_h) {
+            float top = -INFINITY, sum = 0.f;
 #pragma unroll
-          for (int w = 0; w < kWarps; ++w) {
-            const float mw = ml[(w * 8 + h) * 2], f = mw == top ? 1.f : fast_exp2(mw - top);
-            const float4 y = *reinterpret_cast<const float4*>(merge + (w * 8 + h) * Z::kPad + d);
-            sum = __fmaf_rn(ml[(w * 8 + h) * 2 + 1], f, sum);
-            acc.x = __fmaf_rn(y.x, f, acc.x);
-            acc.y = __fmaf_rn(y.y, f, acc.y);
-            acc.z = __fmaf_rn(y.z, f, acc.z);
-            acc.w = __fmaf_rn(y.w, f, acc.w);
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[(w * 8 + h) * 2]);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+              const float mw = ml[(w * 8 + h) * 2], f = mw == top ? 1.f : fast_exp2(mw - top);
+              const float4 y = *reinterpret_cast<const float4*>(merge + (w * 8 + h) * Z::kPad + d);
+              sum = __fmaf_rn(ml[(w * 8 + h) * 2 + 1], f, sum);
+              acc.x = __fmaf_rn(y.x, f, acc.x);
+              acc.y = __fmaf_rn(y.y, f, acc.y);
+              acc.z = __fmaf_rn(y.z, f, acc.z);
+              acc.w = __fmaf_rn(y.w, f, acc.w);
+            }
+            const uint32_t at = 64 * part + d;
+            if (whole) {
+              const float inv = 1.f / sum;
+              T* out = static_cast<T*>(a.out) + (size_t)use.s * a.out_stride + (size_t)(h0 + 8 * nb + h) * D + at;
+              *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
+              if (a.lse && at == 0)
+                a.lse[(size_t)use.s * a.n_heads + h0 + 8 * nb + h] = (top - kOffset + log2f(sum)) * 0.693147180559945309f;
+            } else {
+              *reinterpret_cast<float4*>(sp.part_o + ((size_t)slot * kH + 8 * nb + h) * D + at) = acc;
+              if (at == 0) *reinterpret_cast<float2*>(sp.part_ml + ((size_t)slot * kH + 8 * nb + h) * 2) = make_float2(top, sum);
+            }
           }
-          if (whole) {
-            const float inv = 1.f / sum;
-            T* out = static_cast<T*>(a.out) + (size_t)use.s * a.out_stride + (size_t)(h0 + 8 * nb + h) * D + d;
-            *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
-            if (a.lse && d == 0)
-              a.lse[(size_t)use.s * a.n_heads + h0 + 8 * nb + h] = (top - kOffset + log2f(sum)) * 0.693147180559945309f;
-          } else {
-            *reinterpret_cast<float4*>(sp.part_o + ((size_t)slot * kH + 8 * nb + h) * D + d) = acc;
-            if (d == 0) *reinterpret_cast<float2*>(sp.part_ml + ((size_t)slot * kH + 8 * nb + h) * 2) = make_float2(top, sum);
-          }
+          __syncthreads();
         }
-        __syncthreads();
       }
       fresh = true;
     }
@@ -468,67 +496,91 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
   }
 }
 
-// Joins what several blocks hold of one (sequence, kv head, block of query heads), and answers for sequences
-// without keys.
-template <typename T, int D, int NB>
-__global__ void __launch_bounds__(128) decode_join_kernel(const AttnArgs a, const Split sp) {
-  constexpr int kH = 8 * NB;
-  const uint32_t s = blockIdx.x / sp.hh, hh = blockIdx.x % sp.hh;
-  const uint32_t h0 = hh / sp.ng * a.group + hh % sp.ng * kH, n_h = min((uint32_t)kH, a.group - hh % sp.ng * kH);
+// Joins what several blocks hold of one query head, and answers for sequences without keys.  A block a head: its
+// threads take every fourth or eighth part, 16 bytes of the row each, so that parts arrive side by side.
+constexpr int kJoinThreads = 128;
+template <typename T, int kTile, int D, int NB>
+__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArgs a, const Split sp) {
+  constexpr uint32_t kH = 8 * NB, kVec = D / 4, kWays = kJoinThreads / kVec;
+  const uint32_t s = blockIdx.x / sp.hh, hh = blockIdx.x % sp.hh, h = blockIdx.y;
+  if (h >= a.group - hh % sp.ng * kH) { wait_primary(); return; }
+  const uint32_t head = hh / sp.ng * a.group + hh % sp.ng * kH + h;
+  const uint32_t way = threadIdx.x / kVec, d = threadIdx.x % kVec * 4;
   __shared__ unsigned long long sums[2][4];
+  __shared__ float red[4], part[kWays][D + 1];
   uint64_t before = 0, total = 0;
-  for (uint32_t x = threadIdx.x; x < a.b.n_seqs; x += 128) {
-    const uint32_t n = tiles_of(a.b, x);
+  for (uint32_t x = threadIdx.x; x < a.b.n_seqs; x += kJoinThreads) {
+    const uint32_t n = tiles_of<kTile>(a.b, x);
     total += n;
     if (x < s) before += n;
   }
 #pragma unroll
-  for (int d = 16; d; d /= 2) {
-    total += __shfl_xor_sync(0xffffffffu, total, d);
-    before += __shfl_xor_sync(0xffffffffu, before, d);
+  for (int i = 16; i; i /= 2) {
+    total += __shfl_xor_sync(0xffffffffu, total, i);
+    before += __shfl_xor_sync(0xffffffffu, before, i);
   }
   if (threadIdx.x % 32 == 0) { sums[0][threadIdx.x / 32] = before; sums[1][threadIdx.x / 32] = total; }
   __syncthreads();
   before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
   total = (sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3]) * sp.hh;
-  const uint32_t nt = tiles_of(a.b, s);
+  const uint32_t nt = tiles_of<kTile>(a.b, s);
   const uint32_t n = pieces(total, sp.grid);
+  T* out = static_cast<T*>(a.out) + (size_t)s * a.out_stride + (size_t)head * D + d;
+  float* lse = a.lse ? a.lse + (size_t)s * a.n_heads + head : nullptr;
   wait_primary();
   if (nt == 0) {
     const bool ok = kv_len_ok(a.b, a.b.kv_len[s]);
     if (!ok && threadIdx.x == 0) report(a.b.status, GORGO_KV_BAD_LENGTH);
     const uint32_t none = pack2(ok ? 0.f : NAN, ok ? 0.f : NAN, T());
-    for (uint32_t x = threadIdx.x; x < n_h * (D / 4); x += 128)
-      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (size_t)s * a.out_stride + (size_t)(h0 + x / (D / 4)) * D + x % (D / 4) * 4) =
-          make_uint2(none, none);
-    if (a.lse && threadIdx.x < n_h) a.lse[(size_t)s * a.n_heads + h0 + threadIdx.x] = ok ? -INFINITY : NAN;
+    if (way == 0) *reinterpret_cast<uint2*>(out) = make_uint2(none, none);
+    if (lse && threadIdx.x == 0) *lse = ok ? -INFINITY : NAN;
     return;
   }
   const uint64_t lo = before * sp.hh + (uint64_t)hh * nt, hi = lo + nt;   // its tiles on the line
   const uint32_t c0 = (uint32_t)(((lo + 1) * n - 1) / total), c1 = (uint32_t)((hi * n - 1) / total);   // blocks that hold them
   if (c0 == c1) return;
-  for (uint32_t x = threadIdx.x; x < n_h * (D / 4); x += 128) {
-    const uint32_t h = x / (D / 4), d = x % (D / 4) * 4;
-    float top = -INFINITY, sum = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t c = c0; c <= c1; ++c) {
-      const size_t at = (size_t)(2 * c + (c == c0 ? 1 : 0)) * kH + h;
-      const float2 p = *reinterpret_cast<const float2*>(sp.part_ml + at * 2);
-      const float4 y = *reinterpret_cast<const float4*>(sp.part_o + at * D + d);
-      const float now = fmaxf(top, p.x);
-      const float f = now == top ? 1.f : fast_exp2(top - now), w = p.x == now ? 1.f : fast_exp2(p.x - now);
-      top = now;
-      sum = __fmaf_rn(sum, f, p.y * w);
-      acc.x = __fmaf_rn(acc.x, f, y.x * w);
-      acc.y = __fmaf_rn(acc.y, f, y.y * w);
-      acc.z = __fmaf_rn(acc.z, f, y.z * w);
-      acc.w = __fmaf_rn(acc.w, f, y.w * w);
-    }
-    const float inv = 1.f / sum;
-    T* out = static_cast<T*>(a.out) + (size_t)s * a.out_stride + (size_t)(h0 + h) * D + d;
-    *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
-    if (a.lse && d == 0) a.lse[(size_t)s * a.n_heads + h0 + h] = (top - kOffset + log2f(sum)) * 0.693147180559945309f;
+  // the first block holds its last piece of line, the others their first
+  auto at = [&](uint32_t c) { return (size_t)(2 * c + (c == c0 ? 1 : 0)) * kH + h; };
+  float top = -INFINITY;
+  for (uint32_t c = c0 + threadIdx.x; c <= c1; c += kJoinThreads) top = fmaxf(top, sp.part_ml[at(c) * 2]);
+#pragma unroll
+  for (int i = 16; i; i /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  float sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (uint32_t c = c0 + way; c <= c1; c += kWays) {
+    const float2 p = *reinterpret_cast<const float2*>(sp.part_ml + at(c) * 2);
+    const float4 y = *reinterpret_cast<const float4*>(sp.part_o + at(c) * D + d);
+    const float w = p.x == top ? 1.f : fast_exp2(p.x - top);
+    sum = __fmaf_rn(p.y, w, sum);
+    acc.x = __fmaf_rn(y.x, w, acc.x);
+    acc.y = __fmaf_rn(y.y, w, acc.y);
+    acc.z = __fmaf_rn(y.z, w, acc.z);
+    acc.w = __fmaf_rn(y.w, w, acc.w);
   }
+  part[way][d] = acc.x;
+  part[way][d + 1] = acc.y;
+  part[way][d + 2] = acc.z;
+  part[way][d + 3] = acc.w;
+  if (d == 0) part[way][D] = sum;
+  __syncthreads();
+  if (way) return;
+#pragma unroll
+  for (uint32_t w = 1; w < kWays; ++w) {
+    acc.x += part[w][d];
+    acc.y += part[w][d + 1];
+    acc.z += part[w][d + 2];
+    acc.w += part[w][d + 3];
+  }
+  sum = 0.f;
+#pragma unroll
+  for (uint32_t w = 0; w < kWays; ++w) sum += part[w][D];
+  const float inv = 1.f / sum;
+  *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
+  if (lse && d == 0) *lse = (top - kOffset + log2f(sum)) * 0.693147180559945309f;
 }
 
 uint32_t head_blocks(uint32_t group) { return group <= 8 ? 1 : (group + 15) / 16; }
@@ -541,27 +593,28 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   sp.ng = head_blocks(a.group);
   sp.hh = a.kv.n_kv_heads * sp.ng;
   sp.grid = 2 * sms;
+  sp.box = min((uint32_t)Z::kSlice, 1u << a.kv.page_shift);
   sp.part_o = static_cast<float*>(a.workspace);
   sp.part_ml = sp.part_o + (size_t)2 * sp.grid * 8 * NB * D;
   CUtensorMap km, vm;
   const uint64_t rows = (uint64_t)a.kv.n_pages * a.kv.n_kv_heads << a.kv.page_shift;
-  if (!make_pool_map(&km, a.kv.k, rows, D, a.store, kSlice) || !make_pool_map(&vm, a.kv.v, rows, D, a.store, kSlice))
+  if (!make_pool_map(&km, a.kv.k, rows, D, a.store, sp.box) || !make_pool_map(&vm, a.kv.v, rows, D, a.store, sp.box))
     return cudaErrorUnknown;
   auto kernel = decode_kernel<T, kQuant, D, NB>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Z::kBytes);
+  cudaError_t e = allow_smem<decode_kernel<T, kQuant, D, NB>>(Z::kBytes);
   if (e != cudaSuccess) return e;
   kernel<<<sp.grid, kThreads, Z::kBytes, st>>>(a, sp, km, vm);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.b.n_seqs * sp.hh);
-  cfg.blockDim = dim3(128);
+  cfg.gridDim = dim3(a.b.n_seqs * sp.hh, a.group < 8 * NB ? a.group : 8 * NB);
+  cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
   cudaLaunchAttribute early = {};
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, D, NB>, a, sp);
+  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, Z::kTile, D, NB>, a, sp);
 }
 
 template <typename T, bool kQuant, int D>

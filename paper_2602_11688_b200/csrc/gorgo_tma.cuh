@@ -1,6 +1,8 @@
 // Bulk copies, barriers in shared memory and matrix instructions as the attention kernels use them, and the maps
 // that describe a pool of pages to the copy engine.
 #pragma once
+#include <atomic>
+
 #include "gorgo_attn.cuh"
 
 namespace gorgo {
@@ -11,6 +13,18 @@ namespace gorgo {
 bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t head_dim, uint32_t type, uint32_t box_rows);
 
 #ifdef __CUDACC__
+
+// Lets a kernel have `bytes` of shared memory on the current device (once: the setting stays).
+template <auto kKernel>
+inline cudaError_t allow_smem(int bytes) {
+  static std::atomic<uint64_t> done{0};   // a bit a device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1))) return e;
+  e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kKernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return e;
+}
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
