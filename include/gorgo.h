@@ -524,7 +524,8 @@ typedef struct gorgo_kv_batch {
   uint32_t total_new;           /* rows of the packed array, >= cu_new[n_seqs], < 2^24              */
   uint32_t max_new;             /* most new tokens of one sequence                                 */
   uint32_t max_kv;              /* most tokens of one sequence, < 2^24                             */
-  uint64_t total_kv;            /* bound of the sum of kv_len                                      */
+  uint64_t total_kv;            /* bound of the sum of kv_len, < 2^40 (prefill on e4m3 pages: the sum,  */
+                                /* each length rounded up to 128, times n_kv_heads < 2^31)         */
   uint32_t table_stride;        /* entries from one row of the table to the next; table_stride *   */
                                 /* page_tokens >= max_kv                                           */
   uint32_t reserved;            /* must be 0                                                       */

@@ -572,6 +572,8 @@ class GorgoKvCache:
                                         or e.device != k.device)):
                 raise ValueError("k_exp and v_exp: contiguous int8 [pages, kv heads, page tokens] beside an e4m3 cache")
         self.torch, self.k, self.v, self.k_exp, self.v_exp = torch, k, v, k_exp, v_exp
+        self._raw_stream = torch._C._cuda_getCurrentRawStream   # current_stream(...).cuda_stream without an object
+        self._lib = load()
         self.dtype, self.device = k.dtype, k.device
         self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
         self.c = gorgo_kv_cache_t(k.data_ptr(), v.data_ptr(), _dev_ptr(k_exp), _dev_ptr(v_exp), self.n_pages,
@@ -590,14 +592,16 @@ class GorgoKvCache:
         return cls(*pools, *exps)
 
     def _rows(self, x, n, heads, what):
-        if x.dim() != 3 or x.shape[0] < n or x.shape[1] != heads or x.shape[2] != self.head_dim or \
-                x.device != self.device or x.stride(2) != 1 or x.stride(1) != self.head_dim or x.dtype not in self._types:
+        """The C type of rows [n or more, heads, head dim] whose heads lie one after the other."""
+        shape, strides, t = x.shape, x.stride(), self._types.get(x.dtype)
+        if t is None or len(shape) != 3 or shape[0] < n or shape[1] != heads or shape[2] != self.head_dim or \
+                strides[2] != 1 or strides[1] != shape[2] or x.device != self.device:
             raise ValueError(f"{what}: [{n} rows or more, {heads} heads, {self.head_dim}] in 16 bits on the cache's GPU, "
                              "the heads of a row one after the other")
-        return self._types[x.dtype]
+        return t
 
     def _stream(self):
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+        return self._raw_stream(self.device.index)
 
     def write(self, batch, k_new, v_new):
         """Keys and values [new tokens, kv heads, head dim] of the batch's new tokens into their pages."""
@@ -635,7 +639,7 @@ class GorgoKvCache:
         return self._attend(batch, q, scale, out, lse, batch.n_seqs, 1)
 
     def _attend(self, batch, q, scale, out, lse, rows, decode):
-        torch = self.torch
+        torch, lib = self.torch, self._lib
         heads = q.shape[1] if q.dim() == 3 else 0
         t = self._rows(q, rows, heads, "q")
         if out is None:
@@ -645,17 +649,18 @@ class GorgoKvCache:
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.dim() != 2 or
                                 lse.shape[0] < rows or lse.shape[1] != heads or lse.device != self.device):
             raise ValueError("lse: contiguous float32 [rows, heads] on the cache's GPU")
-        lib, need = load(), C.c_uint64()
-        name = "gorgo_attn_decode" if decode else "gorgo_attn_prefill"
+        need = C.c_uint64()
         rc = lib.gorgo_attn_workspace_bytes(self.ptr, batch.ptr, heads, t, decode, C.byref(need))
+        ws, n = None, need.value
+        if rc == GORGO_OK:
+            if n:
+                ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            rc = (lib.gorgo_attn_decode if decode else lib.gorgo_attn_prefill)(
+                self.ptr, batch.ptr, q.data_ptr(), heads, t, _row_stride(q),
+                self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), _row_stride(out),
+                None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), n, self._stream())
         if rc != GORGO_OK:
-            raise GorgoError(rc, name)
-        ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
-        rc = getattr(lib, name)(self.ptr, batch.ptr, q.data_ptr(), heads, t, _row_stride(q),
-                                self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), _row_stride(out),
-                                _dev_ptr(lse), _dev_ptr(ws), need.value, self._stream())
-        if rc != GORGO_OK:
-            raise GorgoError(rc, name)
+            raise GorgoError(rc, "gorgo_attn_decode" if decode else "gorgo_attn_prefill")
         return out
 
 

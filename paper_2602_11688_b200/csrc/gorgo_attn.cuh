@@ -60,8 +60,9 @@ struct AttnArgs {
   void* workspace;
 };
 uint64_t decode_workspace(const AttnArgs& a, int sms);
-uint64_t attn_workspace(const AttnArgs& a, bool decode, int sms);
-cudaError_t launch_attn_prefill(const AttnArgs& a, cudaStream_t st);
+bool prefill_fits(const AttnArgs& a);           // whether the 16-bit copy of e4m3 pages has fewer than 2^31 rows
+uint64_t prefill_workspace(const AttnArgs& a, int sms);
+cudaError_t launch_attn_prefill(const AttnArgs& a, int sms, cudaStream_t st);
 cudaError_t launch_attn_decode(const AttnArgs& a, int sms, cudaStream_t st);
 
 #ifdef __CUDACC__

@@ -8,10 +8,14 @@ using namespace gorgo;
 
 namespace gorgo {
 
-bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t head_dim, uint32_t type, uint32_t box_rows) {
-  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+namespace {
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool encode3(CUtensorMap* map, uint32_t type, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+             const cuuint32_t* box) {
   static const Encode encode = [] {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found;
@@ -20,17 +24,32 @@ bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t h
       fn = nullptr;
     return reinterpret_cast<Encode>(fn);
   }();
-  if (!encode) return false;
+  const cuuint32_t step[3] = {1, 1, 1};
+  const CUtensorMapDataType t = type == GORGO_E4M3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                : type == GORGO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encode && encode(map, t, 3, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          box[0] * (type == GORGO_E4M3 ? 1 : 2) == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t head_dim, uint32_t type, uint32_t box_rows,
+                   uint32_t box_planes) {
   const uint32_t size = type == GORGO_E4M3 ? 1 : 2;
   const uint32_t cols = head_dim * size < 128 ? head_dim : 128 / size;     // elements of a plane's row
   const cuuint64_t dims[3] = {cols, rows, head_dim / cols};
   const cuuint64_t strides[2] = {(cuuint64_t)head_dim * size, (cuuint64_t)cols * size};
-  const cuuint32_t box[3] = {cols, box_rows, head_dim / cols}, step[3] = {1, 1, 1};
-  const CUtensorMapDataType t = type == GORGO_E4M3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
-                                : type == GORGO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  return encode(map, t, 3, const_cast<void*>(pool), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint32_t box[3] = {cols, box_rows, box_planes};
+  return encode3(map, type, pool, dims, strides, box);
+}
+
+bool make_rows_map(CUtensorMap* map, const void* q, uint32_t rows, uint32_t n_heads, uint32_t head_dim, uint64_t stride,
+                   uint32_t type, uint32_t box_rows, uint32_t box_heads) {
+  const cuuint64_t dims[3] = {head_dim, n_heads, rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64, box_heads, box_rows};
+  return encode3(map, type, q, dims, strides, box);
 }
 
 }  // namespace gorgo
@@ -65,6 +84,7 @@ bool cache_ok(const gorgo_kv_cache_t* c) {
 bool batch_ok(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, bool decode) {
   if (!b || b->reserved || b->n_seqs > 65535) return false;
   if (b->n_seqs == 0) return true;
+  if (b->total_kv >= 1ull << 40) return false;
   if (!b->kv_len || !b->table || (!decode && !b->cu_new)) return false;
   if (!decode && (b->total_new >= (1u << 24) || b->max_new > b->total_new)) return false;
   return b->max_kv < (1u << 24) && (uint64_t)b->table_stride * c->page_tokens >= b->max_kv;
@@ -137,7 +157,8 @@ int attend(bool decode, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, co
   const int sms = dev.ok ? sm_count(c->device) : 0;
   if (!sms) return GORGO_ERR_CUDA;
   AttnArgs a = attn_args(c, b, n_heads, type);
-  const uint64_t need = attn_workspace(a, decode, sms);
+  if (!decode && !prefill_fits(a)) return GORGO_ERR_INVALID_ARG;
+  const uint64_t need = (decode ? decode_workspace(a, sms) : prefill_workspace(a, sms));
   if (need && (!ws || !aligned(ws, 256))) return GORGO_ERR_INVALID_ARG;
   if (ws_bytes < need) return GORGO_ERR_WORKSPACE_TOO_SMALL;
   a.q = q;
@@ -148,7 +169,7 @@ int attend(bool decode, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, co
   a.scale_log2 = (float)(scale * 1.4426950408889634074);
   a.workspace = ws;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return (decode ? launch_attn_decode(a, sms, st) : launch_attn_prefill(a, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
+  return (decode ? launch_attn_decode(a, sms, st) : launch_attn_prefill(a, sms, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
 }
 
 }  // namespace
@@ -174,7 +195,9 @@ int gorgo_attn_workspace_bytes(const gorgo_kv_cache_t* cache, const gorgo_kv_bat
   if (batch->n_seqs == 0) return GORGO_OK;
   const int sms = sm_count(cache->device);
   if (!sms) return GORGO_ERR_CUDA;
-  *bytes_out = attn_workspace(attn_args(cache, batch, n_heads, type), decode != 0, sms);
+  const AttnArgs a = attn_args(cache, batch, n_heads, type);
+  if (!decode && !prefill_fits(a)) return GORGO_ERR_INVALID_ARG;
+  *bytes_out = decode ? decode_workspace(a, sms) : prefill_workspace(a, sms);
   return GORGO_OK;
 }
 

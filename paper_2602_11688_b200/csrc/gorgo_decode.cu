@@ -598,7 +598,9 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   sp.part_ml = sp.part_o + (size_t)2 * sp.grid * 8 * NB * D;
   CUtensorMap km, vm;
   const uint64_t rows = (uint64_t)a.kv.n_pages * a.kv.n_kv_heads << a.kv.page_shift;
-  if (!make_pool_map(&km, a.kv.k, rows, D, a.store, sp.box) || !make_pool_map(&vm, a.kv.v, rows, D, a.store, sp.box))
+  const uint32_t planes = Z::kRow > 128 ? Z::kRow / 128 : 1;
+  if (!make_pool_map(&km, a.kv.k, rows, D, a.store, sp.box, planes) ||
+      !make_pool_map(&vm, a.kv.v, rows, D, a.store, sp.box, planes))
     return cudaErrorUnknown;
   auto kernel = decode_kernel<T, kQuant, D, NB>;
   cudaError_t e = allow_smem<decode_kernel<T, kQuant, D, NB>>(Z::kBytes);

@@ -10,7 +10,12 @@ namespace gorgo {
 // Describes a pool as [rows][D] in pieces of `box_rows` rows: 128-byte columns (64 for 64-element e4m3 rows) so
 // that the copy lays them out with the swizzle of that width; columns of one row follow one another as planes.
 // Rows are counted through the whole pool: (page * n_kv_heads + head) * page_tokens + slot.
-bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t head_dim, uint32_t type, uint32_t box_rows);
+bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t head_dim, uint32_t type, uint32_t box_rows,
+                   uint32_t box_planes);
+// Describes packed rows [rows][n_heads][head_dim] of 16-bit elements, `stride` elements from row to row, in pieces of
+// 64 elements x `box_heads` heads x `box_rows` rows.
+bool make_rows_map(CUtensorMap* map, const void* q, uint32_t rows, uint32_t n_heads, uint32_t head_dim, uint64_t stride,
+                   uint32_t type, uint32_t box_rows, uint32_t box_heads);
 
 #ifdef __CUDACC__
 
@@ -64,6 +69,12 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2}], [%4];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(bar) : "memory");
+}
+// the same rows, one plane
+__device__ __forceinline__ void tma_plane(uint32_t dst, const CUtensorMap* map, int row, int plane, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(plane), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"

@@ -96,9 +96,11 @@ class Made:
         far = torch.einsum("hd,khd->hk", q.double().abs(), k.abs()).amax(1) * abs(scale) * (d + 4) * 2.0 ** -22 + 2.0 ** -20
         out = torch.einsum("hk,khd->hd", p, v)
         sizes = torch.einsum("hk,khd->hd", p, v.abs())
+        # fp16: P, at most 2^15, is a multiple of 2^-30 of its largest value or finer below its normal range
+        few = seen * 2.0 ** -31 * v.abs().amax() if self.dtype == FP16 else 0.0
         # P rounded once (u), numerator and denominator each off by `far`, sums over the keys in 32 bits, the output's rounding
         keys = min(seen, 4096) * 2.0 ** -22
-        bound = sizes * (u + 2 * far[:, None] + keys) * (1 + u) + out.abs() * u + 2.0 ** -24 * u
+        bound = sizes * (u + 2 * far[:, None] + keys) * (1 + u) + out.abs() * u + 2.0 ** -24 * u + few
         return out, torch.logsumexp(z, 1), bound
 
     def expected(self, q, scale, decode):
