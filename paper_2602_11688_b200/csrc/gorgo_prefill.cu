@@ -11,7 +11,7 @@
 //
 // A block takes one kv head and two tiles of 128 rows, floor(128 / group) tokens each with all their query heads, so
 // that keys and values serve a whole group and both tiles.  Warps: 0-3 and 4-7 softmax of the tiles, a row a thread
-// (TMEM lane), no shuffles; 8 copies; 9 issues tcgen05.mma, S of one tile while the other is in softmax.  TMEM: S of
+// (TMEM lane), no shuffles; 8 copies; 9 issues tcgen05.mma (10 and 11 only hand in registers), S of one tile while the other is in softmax.  TMEM: S of
 // both tiles (P of 16 bits takes the place of the S it came from, and is the first operand of P V there), O of both.
 // Keys and values come page by page in tiled bulk copies, 128 keys a slot, each as planes of 128-byte rows with
 // the 128-byte swizzle; V is the second operand as it lies (its dims contiguous).
@@ -30,7 +30,7 @@ namespace gorgo {
 
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;            // three warpgroups: registers can be moved between these only
 constexpr int kKeys = 128;                // keys of a tile
 constexpr uint32_t kPlane = kKeys * 128;  // bytes of 128 rows of 128 bytes
 
@@ -39,7 +39,7 @@ struct Sizes {
   static constexpr int kPlanes = D / 64;
   static constexpr int kTile = kPlanes * kPlane;               // bytes of 128 rows of Q, K or V
   static constexpr int kSlots = D == 128 ? 5 : 10;
-  static constexpr int kBars = 2 * kSlots + 8;
+  static constexpr int kBars = 2 * kSlots + 11;
   static constexpr int kBytes = 2 * kTile + kSlots * kTile + 8 * kBars + 128;
   static constexpr int kO = 256;                               // first TMEM column of O; S of tile i begins at 128 i
 };
@@ -211,7 +211,64 @@ __device__ __forceinline__ bool wait_or_give_up(uint32_t bar, uint32_t parity, v
 template <typename T> constexpr float kShift = 0.f;      // P = 2^(c (S - m) + kShift)
 template <> constexpr float kShift<__half> = 6.f;        // fp16: normal down to 2^-20 of the largest, below 2^15
 
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+// The larger of three; NaN if one is.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
+// Two floats in one register pair, and arithmetic on both at once.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 both(float x, float y) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 apart(f32x2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// 2^x for -125 <= x < 100 (below: 2^-125) without the special function unit: 2^n by the exponent, n = x rounded, times
+// a polynomial in x - n, |x - n| <= 1/2.  Its coefficients are the best in relative error, found by Remez exchange: off
+// by at most 7.5e-5 (degree 3, for P in bf16, whose rounding is off by 3.9e-3) or 2.6e-6 (degree 4, fp16: 4.9e-4).
+template <typename T>
+__device__ __forceinline__ float2 poly_exp2(f32x2 x) {
+  constexpr float kRound = 12582912.f;    // 1.5 * 2^23: the sum's low bits are x rounded
+  float2 y = apart(x);
+  y.x = fmaxf(y.x, -125.f);
+  y.y = fmaxf(y.y, -125.f);
+  x = both(y.x, y.y);
+  const f32x2 n = add2(x, both(kRound, kRound));
+  const f32x2 back = add2(n, both(-kRound, -kRound));
+  const f32x2 f = fma2(back, both(-1.f, -1.f), x);
+  f32x2 r;
+  if (std::is_same<T, __half>::value) {
+    r = fma2(f, both(9.570101863e-3f, 9.570101863e-3f), both(5.591786034e-2f, 5.591786034e-2f));
+    r = fma2(f, r, both(2.402474483e-1f, 2.402474483e-1f));
+    r = fma2(f, r, both(6.931218147e-1f, 6.931218147e-1f));
+    r = fma2(f, r, both(9.999992614e-1f, 9.999992614e-1f));
+  } else {
+    r = fma2(f, both(5.517167480e-2f, 5.517167480e-2f), both(2.426111243e-1f, 2.426111243e-1f));
+    r = fma2(f, r, both(6.932609842e-1f, 6.932609842e-1f));
+    r = fma2(f, r, both(9.999280732e-1f, 9.999280732e-1f));
+  }
+  const float2 m = apart(n), z = apart(r);
+  return make_float2(__int_as_float(__float_as_int(z.x) + (__float_as_int(m.x) << 23)),
+                     __int_as_float(__float_as_int(z.y) + (__float_as_int(m.y) << 23)));
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -225,7 +282,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   const uint32_t q_a = smem_u32(smem), ring_a = q_a + 2 * Z::kTile;
   const uint32_t bars = ring_a + Z::kSlots * Z::kTile;
   const uint32_t full = bars, empty = full + 8 * Z::kSlots, q_full = empty + 8 * Z::kSlots, s_full = q_full + 8,
-                 p_full = s_full + 16, o_full = p_full + 16, drained = o_full + 16;
+                 p_full = s_full + 16, o_full = p_full + 32, drained = o_full + 16, tail = drained + 8;
 
   if (warp == 8) {
     Work w;
@@ -241,10 +298,12 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       mbar_init(q_full, 1);
       for (int i = 0; i < 2; ++i) {
         mbar_init(s_full + 8 * i, 1);
-        mbar_init(p_full + 8 * i, 128);
+        mbar_init(p_full + 16 * i, 128);
+        mbar_init(p_full + 16 * i + 8, 128);
         mbar_init(o_full + 8 * i, 1);
       }
       mbar_init(drained, 1);
+      mbar_init(tail, 1);
       mbar_init_fence();
     }
   }
@@ -263,148 +322,12 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   const uint32_t tmem = tmem_base;
   const int steps[2] = {max(0, min(w.hi, w.tiles[0]) - w.lo), max(0, min(w.hi, w.tiles[1]) - w.lo)};
   const int most = max(steps[0], steps[1]);
+  const bool ragged = most > 0 && (w.lo + most) * kKeys > w.kv;  // the last tile of keys is not full
 
-  if (warp == 8) {
-    // ---------------------------------------------------------------- copies
-    if (most > 0) {
-      if (lane == 0) {
-        const uint32_t rows = p.tq * a.group;
-        uint32_t bytes = 0;
-        for (int i = 0; i < 2; ++i) bytes += steps[i] ? Z::kPlanes * rows * 128 : 0;
-        mbar_expect(q_full, bytes);
-        for (int i = 0; i < 2; ++i)
-          for (int c = 0; steps[i] && c < Z::kPlanes; ++c)
-            asm volatile(
-                "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                ::"r"(q_a + i * Z::kTile + c * kPlane), "l"(reinterpret_cast<uint64_t>(&q_map)), "r"(c * 64),
-                "r"((int)(w.h * a.group)), "r"(w.first + w.q0 + i * (int)p.tq), "r"(q_full) : "memory");
-      }
-      // a lane a piece: the piece's page is looked up a tile ahead
-      const uint32_t most_pieces = kKeys / p.box;
-      auto row_of = [&](int j) -> int64_t {
-        const int key = (w.lo + j) * kKeys + (int)(lane * p.box);
-        if (lane >= most_pieces || key >= w.kv) return -2;
-        if (p.linear) return (int64_t)(w.h * p.linear + w.base + key);
-        return pool_row(a.kv, a.b, w.s, w.h, (uint32_t)key);
-      };
-      int64_t row = row_of(0);
-      uint32_t slot = 0, phase = 1, copied = 0;
-      bool go = true;
-      for (int j = 0; go && j < most; ++j) {
-        if (row == -1) {                  // a wrong page: copies something that is there, and says so
-          report(a.b.status, GORGO_KV_BAD_PAGE);
-          work.bad = 1;
-          row = 0;
-        }
-        const uint32_t pieces = __popc(__ballot_sync(0xffffffffu, row >= 0));
-        const int64_t next = j + 1 < most ? row_of(j + 1) : -2;
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          go = __all_sync(0xffffffffu, wait_or_give_up(empty + 8 * slot, phase, &quit, a.b.status));
-          if (!go) break;
-          if (lane == 0) mbar_expect(full + 8 * slot, pieces * p.box * D * 2);
-          __syncwarp();
-          if (row >= 0)
-            for (int c = 0; c < Z::kPlanes; ++c)
-              tma_plane(ring_a + slot * Z::kTile + c * kPlane + lane * p.box * 128, v ? &v_map : &k_map, (int)row, c, full + 8 * slot);
-          ++copied;
-          if (++slot == (uint32_t)Z::kSlots) { slot = 0; phase ^= 1; }
-        }
-        row = next;
-      }
-      if (quit) {                         // what flies has to land before the block ends
-        mbar_wait(q_full, 0);
-        for (uint32_t i = 0; i < min(copied, (uint32_t)Z::kSlots); ++i)
-          mbar_wait(full + 8 * i, i < slot ? phase ^ 1 : phase);         // the last copy into the slot
-      }
-    }
-  } else if (warp == 9) {
-    // ---------------------------------------------------------------- products
-    if (most > 0) {
-      constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
-      const uint32_t s_shape = mma_shape(kKeys, kBf, p.negate != 0, false), o_shape = mma_shape(D, kBf, false, true);
-      auto scores = [&](int i, uint32_t slot) {               // S_i = Q_i K^T
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (k / 4) * kPlane + (k % 4) * 32;
-          mma_ss(tmem + 128 * i, operand(q_a + i * Z::kTile + off, 16), operand(ring_a + slot * Z::kTile + off, 16), s_shape, k > 0);
-        }
-      };
-      auto values = [&](int i, uint32_t slot, bool acc) {      // O_i (+)= P_i V
-#pragma unroll
-        for (int k = 0; k < kKeys / 16; ++k)
-          mma_ts(tmem + Z::kO + D * i, tmem + 128 * i + 8 * k, operand(ring_a + slot * Z::kTile + k * 2048, kPlane), o_shape, acc || k > 0);
-      };
-      bool go = wait_or_give_up(q_full, 0, &quit, a.b.status);
-      uint32_t slot = 0, phase = 0;
-      auto next_slot = [&] {
-        const uint32_t s = slot;
-        if (++slot == (uint32_t)Z::kSlots) { slot = 0; phase ^= 1; }
-        return s;
-      };
-      go = go && wait_or_give_up(full, 0, &quit, a.b.status);
-      go = __all_sync(0xffffffffu, go);
-      uint32_t k_slot = next_slot();
-      if (go && lane == 0) {
-        fence_after();
-        for (int i = 0; i < 2; ++i)
-          if (steps[i]) {
-            scores(i, k_slot);
-            mma_commit(s_full + 8 * i);
-          }
-        mma_commit(empty + 8 * k_slot);
-      }
-      for (int j = 0; go && j < most; ++j) {
-        go = __all_sync(0xffffffffu, wait_or_give_up(full + 8 * slot, phase, &quit, a.b.status));
-        if (!go) break;
-        const uint32_t v_slot = next_slot();
-        const int behind = w.kv - (w.lo + j) * kKeys;          // keys of this tile
-        if (behind < kKeys) {                                  // what lies behind the last becomes zeros
-          for (uint32_t x = lane; x < (uint32_t)(kKeys - behind) * 8 * Z::kPlanes; x += 32) {
-            const uint32_t c = x / ((kKeys - behind) * 8), y = x % ((kKeys - behind) * 8);
-            *reinterpret_cast<uint4*>(smem + 2 * Z::kTile + v_slot * Z::kTile + c * kPlane + behind * 128 + y * 16) = make_uint4(0, 0, 0, 0);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-        }
-        const bool more = j + 1 < most;
-        bool have_k = false;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (j >= steps[i]) continue;
-          go = __all_sync(0xffffffffu, go && wait_or_give_up(p_full + 8 * i, j & 1, &quit, a.b.status));
-          if (!go) break;
-          if (lane == 0) {
-            fence_after();
-            values(i, v_slot, j > 0);
-          }
-          if (j + 1 < steps[i]) {
-            if (!have_k) {
-              go = __all_sync(0xffffffffu, wait_or_give_up(full + 8 * slot, phase, &quit, a.b.status));
-              if (!go) break;
-              k_slot = next_slot();
-              have_k = true;
-            }
-            if (lane == 0) {
-              fence_after();
-              scores(i, k_slot);
-              mma_commit(s_full + 8 * i);
-            }
-          } else if (lane == 0) {
-            mma_commit(o_full + 8 * i);
-          }
-        }
-        if (go && lane == 0) {
-          mma_commit(empty + 8 * v_slot);
-          if (more) mma_commit(empty + 8 * k_slot);
-        }
-      }
-      if (quit) {                         // products in flight end before the block does
-        if (lane == 0) mma_commit(drained);
-        mbar_wait(drained, 0);
-      }
-    }
-  } else {
+  // Registers: 384 threads of 168 at the launch; the softmax takes what the last warpgroup does not need
+  // (2 * 208 + 88 = 3 * 168).
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---------------------------------------------------------------- softmax, a row a thread
     const int i = warp / 4;
     const uint32_t r = warp % 4 * 32 + lane, at = tmem + (warp % 4 * 32 << 16);
@@ -425,7 +348,8 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       for (int k = 0; k < 4; ++k) tmem_ld32(x + 32 * k, s_at + 32 * k);
       tmem_wait_ld();
       const int seen = pos - (w.lo + j) * kKeys + 1;           // columns that the row sees
-      if (__any_sync(0xffffffffu, seen < kKeys)) {
+      const bool masked = __any_sync(0xffffffffu, seen < kKeys);
+      if (masked) {
 #pragma unroll
         for (int k = 0; k < kKeys; ++k)
           if (k >= seen) x[k] = 0xff800000u;
@@ -435,9 +359,10 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       for (int k = 0; k < kKeys; k += 8)
 #pragma unroll
         for (int y = 0; y < 4; ++y) top[y] = max3(top[y], __uint_as_float(x[k + 2 * y]), __uint_as_float(x[k + 2 * y + 1]));
-      const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      const bool grow = now > m + slack;
+      float now = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
+      const bool grow = !(now <= m + slack);                   // (also for NaN)
       if (__any_sync(0xffffffffu, grow)) {
+        if (now == INFINITY) now = NAN;                        // infinity - infinity: the row is NaN
         const float f = grow ? fast_exp2((m - now) * c) : 1.f;
         if (grow) m = now;
         l *= f;
@@ -454,24 +379,40 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         }
       }
       const float off = m == -INFINITY ? 0.f : kShift<T> - m * c;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      // P in halves of 64 keys: their products with V begin while the other half is computed
+      f32x2 sum[4] = {0, 0, 0, 0};
+      const f32x2 c2 = both(c, c), off2 = both(off, off);
+      auto half = [&](int k, auto poly) {
         uint32_t pk[32];
 #pragma unroll
         for (int y = 0; y < 32; ++y) {
-          const float u = fast_exp2(__fmaf_rn(__uint_as_float(x[64 * k + 2 * y]), c, off));
-          const float v = fast_exp2(__fmaf_rn(__uint_as_float(x[64 * k + 2 * y + 1]), c, off));
-          sum[y % 2 * 2] += u;
-          sum[y % 2 * 2 + 1] += v;
-          pk[y] = pack2(u, v, T());
+          const f32x2 z = fma2(both(__uint_as_float(x[64 * k + 2 * y]), __uint_as_float(x[64 * k + 2 * y + 1])), c2, off2);
+          float2 e;
+          if (decltype(poly)::value && y % 4 == 3) {
+            e = poly_exp2<T>(z);
+          } else {
+            e = apart(z);
+            e.x = fast_exp2(e.x);
+            e.y = fast_exp2(e.y);
+          }
+          sum[y % 4] = add2(sum[y % 4], both(e.x, e.y));
+          pk[y] = pack2(e.x, e.y, T());
         }
         tmem_st32(s_at + 32 * k, pk);
+        tmem_wait_st();
+        fence_before();
+        mbar_arrive(p_full + 8 * (2 * i + k));
+      };
+      // a quarter of the exponentials by the polynomial, unless a column is masked (its P has to be 0)
+      if (masked || __any_sync(0xffffffffu, m == -INFINITY)) {
+        half(0, std::false_type());
+        half(1, std::false_type());
+      } else {
+        half(0, std::true_type());
+        half(1, std::true_type());
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tmem_wait_st();
-      fence_before();
-      mbar_arrive(p_full + 8 * i);
+      const float2 l2 = apart(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+      l += l2.x + l2.y;
     }
     if (steps[i] && go) {
       go = __all_sync(0xffffffffu, wait_or_give_up(o_full + 8 * i, 0, &quit, a.b.status));
@@ -530,6 +471,142 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       }
     }
     fence_before();
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 8) {
+      // ---------------------------------------------------------------- copies
+      if (most > 0) {
+        if (lane == 0) {
+          const uint32_t rows = p.tq * a.group;
+          uint32_t bytes = 0;
+          for (int i = 0; i < 2; ++i) bytes += steps[i] ? Z::kPlanes * rows * 128 : 0;
+          mbar_expect(q_full, bytes);
+          for (int i = 0; i < 2; ++i)
+            for (int c = 0; steps[i] && c < Z::kPlanes; ++c)
+              asm volatile(
+                  "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                  ::"r"(q_a + i * Z::kTile + c * kPlane), "l"(reinterpret_cast<uint64_t>(&q_map)), "r"(c * 64),
+                  "r"((int)(w.h * a.group)), "r"(w.first + w.q0 + i * (int)p.tq), "r"(q_full) : "memory");
+        }
+        // a lane a piece: the piece's page is looked up a tile ahead
+        const uint32_t most_pieces = kKeys / p.box;
+        auto row_of = [&](int j) -> int64_t {
+          const int key = (w.lo + j) * kKeys + (int)(lane * p.box);
+          if (lane >= most_pieces || key >= w.kv) return -2;
+          if (p.linear) return (int64_t)(w.h * p.linear + w.base + key);
+          return pool_row(a.kv, a.b, w.s, w.h, (uint32_t)key);
+        };
+        int64_t row = row_of(0);
+        uint32_t slot = 0, phase = 1, copied = 0;
+        bool go = true;
+        for (int j = 0; go && j < most; ++j) {
+          if (row == -1) {                  // a wrong page: copies something that is there, and says so
+            report(a.b.status, GORGO_KV_BAD_PAGE);
+            work.bad = 1;
+            row = 0;
+          }
+          const uint32_t pieces = __popc(__ballot_sync(0xffffffffu, row >= 0));
+          const int64_t next = j + 1 < most ? row_of(j + 1) : -2;
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            go = __all_sync(0xffffffffu, wait_or_give_up(empty + 8 * slot, phase, &quit, a.b.status));
+            if (!go) break;
+            if (lane == 0) mbar_expect(full + 8 * slot, pieces * p.box * D * 2);
+            __syncwarp();
+            if (row >= 0)
+              for (int c = 0; c < Z::kPlanes; ++c)
+                tma_plane(ring_a + slot * Z::kTile + c * kPlane + lane * p.box * 128, v ? &v_map : &k_map, (int)row, c, full + 8 * slot);
+            ++copied;
+            if (++slot == (uint32_t)Z::kSlots) { slot = 0; phase ^= 1; }
+          }
+          row = next;
+        }
+        if (ragged && go) {                 // what lies behind the last key becomes zeros
+          const uint32_t last = copied - 1, at = last % Z::kSlots;
+          if (__all_sync(0xffffffffu, wait_or_give_up(full + 8 * at, last / Z::kSlots & 1, &quit, a.b.status))) {
+            const uint32_t here = w.kv - (w.lo + most - 1) * kKeys, rest = (kKeys - here) * 8;
+            for (uint32_t x = lane; x < rest * Z::kPlanes; x += 32)
+              *reinterpret_cast<uint4*>(smem + 2 * Z::kTile + at * Z::kTile + x / rest * kPlane + here * 128 + x % rest * 16) =
+                  make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tail);
+          }
+        }
+        if (quit) {                         // what flies has to land before the block ends
+          mbar_wait(q_full, 0);
+          for (uint32_t i = 0; i < min(copied, (uint32_t)Z::kSlots); ++i)
+            mbar_wait(full + 8 * i, i < slot ? phase ^ 1 : phase);         // the last copy into the slot
+        }
+      }
+    } else if (warp == 9) {
+      // -------------------------------------------------------------- products: one thread, nothing between two waits
+      // but the issue itself (the tensor pipe takes few instructions ahead, so what this thread does besides shows)
+      if (lane == 0 && most > 0) {
+        constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
+        const uint32_t s_shape = mma_shape(kKeys, kBf, p.negate != 0, false), o_shape = mma_shape(D, kBf, false, true);
+        const uint64_t q_op = operand(q_a, 16), k_op = operand(ring_a, 16), v_op = operand(ring_a, kPlane);
+        auto scores = [&](int i, uint32_t slot) {              // S_i = Q_i K^T
+          const uint64_t x = q_op + i * (Z::kTile >> 4), y = k_op + slot * (Z::kTile >> 4);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = ((k / 4) * kPlane + (k % 4) * 32) >> 4;
+            mma_ss(tmem + 128 * i, x + off, y + off, s_shape, k > 0);
+          }
+          mma_commit(s_full + 8 * i);
+        };
+        auto values = [&](int i, uint32_t slot, int half, bool acc) {   // O_i (+)= P_i V, 64 keys
+          const uint64_t y = v_op + slot * (Z::kTile >> 4);
+#pragma unroll
+          for (int k = 4 * half; k < 4 * half + 4; ++k)
+            mma_ts(tmem + Z::kO + D * i, tmem + 128 * i + 8 * k, y + (k * 2048 >> 4), o_shape, acc || k > 0);
+        };
+        uint32_t slot = 0, phase = 0;
+        auto take = [&](uint32_t bar) {                        // the next slot, when it is there
+          if (!wait_or_give_up(bar, bar == tail ? 0 : phase, &quit, a.b.status)) return false;
+          if (++slot == (uint32_t)Z::kSlots) { slot = 0; phase ^= 1; }
+          return true;
+        };
+        bool go = wait_or_give_up(q_full, 0, &quit, a.b.status) && take(full);
+        if (go) {
+          fence_after();
+          for (int i = 0; i < 2; ++i)
+            if (steps[i]) scores(i, 0);
+          mma_commit(empty);
+        }
+        for (int j = 0; go && j < most; ++j) {
+          const uint32_t v_slot = slot;
+          if (!take(ragged && j + 1 == most ? tail : full + 8 * slot)) break;
+          uint32_t k_slot = slot;
+          bool have_k = false;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (!go || j >= steps[i]) continue;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              go = go && wait_or_give_up(p_full + 8 * (2 * i + k), j & 1, &quit, a.b.status);
+              fence_after();
+              if (go) values(i, v_slot, k, j > 0);
+            }
+            if (j + 1 < steps[i]) {
+              if (!have_k) go = go && take(full + 8 * slot);
+              have_k = true;
+              if (go) scores(i, k_slot);
+            } else if (go) {
+              mma_commit(o_full + 8 * i);
+            }
+          }
+          if (!go) break;
+          mma_commit(empty + 8 * v_slot);
+          if (have_k) mma_commit(empty + 8 * k_slot);
+        }
+        if (quit) {                       // products in flight end before the block does
+          mma_commit(drained);
+          mbar_wait(drained, 0);
+        }
+      }
+      __syncwarp();
+    }
   }
   __syncthreads();
   fence_after();
