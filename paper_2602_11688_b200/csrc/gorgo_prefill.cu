@@ -78,17 +78,23 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// Operands in shared memory, rows of 128 bytes in the 128-byte swizzle, groups of 8 rows 1,024 bytes apart: the low word
+// has the address and `lead`, the bytes from one 64-element plane to the next where the rows run along the summed
+// dimension (V; else unused), in units of 16; the high word is the same for all.
+constexpr uint32_t kOperandHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t lead) { return addr >> 4 | (lead >> 4) << 16; }
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 x, {%1, %3};\n\tmov.b64 y, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "n"(kOperandHigh), "r"(shape), "r"(acc) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 y, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "n"(kOperandHigh), "r"(shape), "r"(acc) : "memory");
 }
 #define GORGO_R32(r, o)                                                                                              \
   "=r"((r)[(o) + 0]), "=r"((r)[(o) + 1]), "=r"((r)[(o) + 2]), "=r"((r)[(o) + 3]), "=r"((r)[(o) + 4]),                \
@@ -116,14 +122,15 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
       "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
       ::GORGO_I32(r), "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Operands in shared memory, rows of 128 bytes in the 128-byte swizzle, groups of 8 rows 1,024 bytes apart; `lead`: bytes
-// from one 64-element plane to the next where the rows run along the summed dimension (V), else unused.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
 // 128 x n product of 16-bit operands, summed in 32 bits.
 __device__ __forceinline__ uint32_t mma_shape(uint32_t n, bool bf16, bool negate_a, bool b_by_rows) {
   return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (negate_a ? 1u << 13 : 0u) | (b_by_rows ? 1u << 16 : 0u) |
@@ -325,9 +332,9 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   const bool ragged = most > 0 && (w.lo + most) * kKeys > w.kv;  // the last tile of keys is not full
 
   // Registers: 384 threads of 168 at the launch; the softmax takes what the last warpgroup does not need
-  // (2 * 208 + 88 = 3 * 168).
+  // (2 * 200 + 104 = 3 * 168).
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     // ---------------------------------------------------------------- softmax, a row a thread
     const int i = warp / 4;
     const uint32_t r = warp % 4 * 32 + lane, at = tmem + (warp % 4 * 32 << 16);
@@ -343,22 +350,27 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       go = __all_sync(0xffffffffu, wait_or_give_up(s_full + 8 * i, j & 1, &quit, a.b.status));
       if (!go) break;
       fence_after();
-      uint32_t x[128];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) tmem_ld32(x + 32 * k, s_at + 32 * k);
-      tmem_wait_ld();
       const int seen = pos - (w.lo + j) * kKeys + 1;           // columns that the row sees
       const bool masked = __any_sync(0xffffffffu, seen < kKeys);
-      if (masked) {
+      // Half of a row at a time: the second half is read twice, which costs less than the registers for all of it.
+      uint32_t x[64];
+      auto read = [&](int k) {
+        tmem_ld32(x, s_at + 64 * k);
+        tmem_ld32(x + 32, s_at + 64 * k + 32);
+        tmem_wait_ld();
+        if (masked) {
 #pragma unroll
-        for (int k = 0; k < kKeys; ++k)
-          if (k >= seen) x[k] = 0xff800000u;
-      }
+          for (int y = 0; y < 64; ++y)
+            if (64 * k + y >= seen) x[y] = 0xff800000u;
+        }
+      };
       float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int k = 0; k < kKeys; k += 8)
+      for (int k = 1; k >= 0; --k) {
+        read(k);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) top[y] = max3(top[y], __uint_as_float(x[k + 2 * y]), __uint_as_float(x[k + 2 * y + 1]));
+        for (int y = 0; y < 64; y += 2) top[y / 2 % 4] = max3(top[y / 2 % 4], __uint_as_float(x[y]), __uint_as_float(x[y + 1]));
+      }
       float now = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
       const bool grow = !(now <= m + slack);                   // (also for NaN)
       if (__any_sync(0xffffffffu, grow)) {
@@ -383,22 +395,25 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       f32x2 sum[4] = {0, 0, 0, 0};
       const f32x2 c2 = both(c, c), off2 = both(off, off);
       auto half = [&](int k, auto poly) {
-        uint32_t pk[32];
 #pragma unroll
-        for (int y = 0; y < 32; ++y) {
-          const f32x2 z = fma2(both(__uint_as_float(x[64 * k + 2 * y]), __uint_as_float(x[64 * k + 2 * y + 1])), c2, off2);
-          float2 e;
-          if (decltype(poly)::value && y % 4 == 3) {
-            e = poly_exp2<T>(z);
-          } else {
-            e = apart(z);
-            e.x = fast_exp2(e.x);
-            e.y = fast_exp2(e.y);
+        for (int q = 0; q < 2; ++q) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int y = 0; y < 16; ++y) {
+            const f32x2 z = fma2(both(__uint_as_float(x[32 * q + 2 * y]), __uint_as_float(x[32 * q + 2 * y + 1])), c2, off2);
+            float2 e;
+            if (decltype(poly)::value && y % 4 == 3) {
+              e = poly_exp2<T>(z);
+            } else {
+              e = apart(z);
+              e.x = fast_exp2(e.x);
+              e.y = fast_exp2(e.y);
+            }
+            sum[y % 4] = add2(sum[y % 4], both(e.x, e.y));
+            pk[y] = pack2(e.x, e.y, T());
           }
-          sum[y % 4] = add2(sum[y % 4], both(e.x, e.y));
-          pk[y] = pack2(e.x, e.y, T());
+          tmem_st16(s_at + 32 * k + 16 * q, pk);
         }
-        tmem_st32(s_at + 32 * k, pk);
         tmem_wait_st();
         fence_before();
         mbar_arrive(p_full + 8 * (2 * i + k));
@@ -406,9 +421,11 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       // a quarter of the exponentials by the polynomial, unless a column is masked (its P has to be 0)
       if (masked || __any_sync(0xffffffffu, m == -INFINITY)) {
         half(0, std::false_type());
+        read(1);
         half(1, std::false_type());
       } else {
         half(0, std::true_type());
+        read(1);
         half(1, std::true_type());
       }
       const float2 l2 = apart(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
@@ -472,7 +489,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
     }
     fence_before();
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 8) {
       // ---------------------------------------------------------------- copies
       if (most > 0) {
@@ -545,9 +562,9 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       if (lane == 0 && most > 0) {
         constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
         const uint32_t s_shape = mma_shape(kKeys, kBf, p.negate != 0, false), o_shape = mma_shape(D, kBf, false, true);
-        const uint64_t q_op = operand(q_a, 16), k_op = operand(ring_a, 16), v_op = operand(ring_a, kPlane);
+        const uint32_t q_op = operand(q_a, 16), k_op = operand(ring_a, 16), v_op = operand(ring_a, kPlane);
         auto scores = [&](int i, uint32_t slot) {              // S_i = Q_i K^T
-          const uint64_t x = q_op + i * (Z::kTile >> 4), y = k_op + slot * (Z::kTile >> 4);
+          const uint32_t x = q_op + i * (Z::kTile >> 4), y = k_op + slot * (Z::kTile >> 4);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint32_t off = ((k / 4) * kPlane + (k % 4) * 32) >> 4;
@@ -556,7 +573,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
           mma_commit(s_full + 8 * i);
         };
         auto values = [&](int i, uint32_t slot, int half, bool acc) {   // O_i (+)= P_i V, 64 keys
-          const uint64_t y = v_op + slot * (Z::kTile >> 4);
+          const uint32_t y = v_op + slot * (Z::kTile >> 4);
 #pragma unroll
           for (int k = 4 * half; k < 4 * half + 4; ++k)
             mma_ts(tmem + Z::kO + D * i, tmem + 128 * i + 8 * k, y + (k * 2048 >> 4), o_shape, acc || k > 0);
