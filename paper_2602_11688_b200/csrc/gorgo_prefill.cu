@@ -66,6 +66,12 @@ struct Work {                             // what a block does
 };
 
 // ------------------------------------------------------------------ tcgen05
+// One thread of a converged warp; the compiler knows that what follows runs alone and keeps operands in uniform registers.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
 __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t cols) {
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
   asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -248,35 +254,6 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   return r;
 }
 
-// 2^x for -125 <= x < 100 (below: 2^-125) without the special function unit: 2^n by the exponent, n = x rounded, times
-// a polynomial in x - n, |x - n| <= 1/2.  Its coefficients are the best in relative error, found by Remez exchange: off
-// by at most 7.5e-5 (degree 3, for P in bf16, whose rounding is off by 3.9e-3) or 2.6e-6 (degree 4, fp16: 4.9e-4).
-template <typename T>
-__device__ __forceinline__ float2 poly_exp2(f32x2 x) {
-  constexpr float kRound = 12582912.f;    // 1.5 * 2^23: the sum's low bits are x rounded
-  float2 y = apart(x);
-  y.x = fmaxf(y.x, -125.f);
-  y.y = fmaxf(y.y, -125.f);
-  x = both(y.x, y.y);
-  const f32x2 n = add2(x, both(kRound, kRound));
-  const f32x2 back = add2(n, both(-kRound, -kRound));
-  const f32x2 f = fma2(back, both(-1.f, -1.f), x);
-  f32x2 r;
-  if (std::is_same<T, __half>::value) {
-    r = fma2(f, both(9.570101863e-3f, 9.570101863e-3f), both(5.591786034e-2f, 5.591786034e-2f));
-    r = fma2(f, r, both(2.402474483e-1f, 2.402474483e-1f));
-    r = fma2(f, r, both(6.931218147e-1f, 6.931218147e-1f));
-    r = fma2(f, r, both(9.999992614e-1f, 9.999992614e-1f));
-  } else {
-    r = fma2(f, both(5.517167480e-2f, 5.517167480e-2f), both(2.426111243e-1f, 2.426111243e-1f));
-    r = fma2(f, r, both(6.932609842e-1f, 6.932609842e-1f));
-    r = fma2(f, r, both(9.999280732e-1f, 9.999280732e-1f));
-  }
-  const float2 m = apart(n), z = apart(r);
-  return make_float2(__int_as_float(__float_as_int(z.x) + (__float_as_int(m.x) << 23)),
-                     __int_as_float(__float_as_int(z.y) + (__float_as_int(m.y) << 23)));
-}
-
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan p, const __grid_constant__ CUtensorMap q_map,
@@ -359,9 +336,10 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         tmem_ld32(x + 32, s_at + 64 * k + 32);
         tmem_wait_ld();
         if (masked) {
+          const int left = seen - 64 * k;
 #pragma unroll
           for (int y = 0; y < 64; ++y)
-            if (64 * k + y >= seen) x[y] = 0xff800000u;
+            if (y >= left) x[y] = 0xff800000u;
         }
       };
       float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -394,21 +372,17 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       // P in halves of 64 keys: their products with V begin while the other half is computed
       f32x2 sum[4] = {0, 0, 0, 0};
       const f32x2 c2 = both(c, c), off2 = both(off, off);
-      auto half = [&](int k, auto poly) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (k) read(1);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t pk[16];
 #pragma unroll
           for (int y = 0; y < 16; ++y) {
-            const f32x2 z = fma2(both(__uint_as_float(x[32 * q + 2 * y]), __uint_as_float(x[32 * q + 2 * y + 1])), c2, off2);
-            float2 e;
-            if (decltype(poly)::value && y % 4 == 3) {
-              e = poly_exp2<T>(z);
-            } else {
-              e = apart(z);
-              e.x = fast_exp2(e.x);
-              e.y = fast_exp2(e.y);
-            }
+            float2 e = apart(fma2(both(__uint_as_float(x[32 * q + 2 * y]), __uint_as_float(x[32 * q + 2 * y + 1])), c2, off2));
+            e.x = fast_exp2(e.x);
+            e.y = fast_exp2(e.y);
             sum[y % 4] = add2(sum[y % 4], both(e.x, e.y));
             pk[y] = pack2(e.x, e.y, T());
           }
@@ -417,16 +391,6 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         tmem_wait_st();
         fence_before();
         mbar_arrive(p_full + 8 * (2 * i + k));
-      };
-      // a quarter of the exponentials by the polynomial, unless a column is masked (its P has to be 0)
-      if (masked || __any_sync(0xffffffffu, m == -INFINITY)) {
-        half(0, std::false_type());
-        read(1);
-        half(1, std::false_type());
-      } else {
-        half(0, std::true_type());
-        read(1);
-        half(1, std::true_type());
       }
       const float2 l2 = apart(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
       l += l2.x + l2.y;
@@ -559,7 +523,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
     } else if (warp == 9) {
       // -------------------------------------------------------------- products: one thread, nothing between two waits
       // but the issue itself (the tensor pipe takes few instructions ahead, so what this thread does besides shows)
-      if (lane == 0 && most > 0) {
+      if (most > 0 && elect_one()) {
         constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
         const uint32_t s_shape = mma_shape(kKeys, kBf, p.negate != 0, false), o_shape = mma_shape(D, kBf, false, true);
         const uint32_t q_op = operand(q_a, 16), k_op = operand(ring_a, 16), v_op = operand(ring_a, kPlane);

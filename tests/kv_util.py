@@ -92,10 +92,8 @@ class Made:
         z = torch.einsum("hd,khd->hk", q.double(), k) * scale
         p = torch.softmax(z, 1)
         # a score's error: `dim` products summed in 32 bits, each step off by at most 2^-22 of the sum of sizes (the
-        # matrix unit cuts where it aligns), its product with the scale, the exponential (2^-21, or a polynomial that is off
-        # by at most 7.5e-5 in bf16 and 2.6e-6 in fp16)
-        far = torch.einsum("hd,khd->hk", q.double().abs(), k.abs()).amax(1) * abs(scale) * (d + 4) * 2.0 ** -22 + 2.0 ** -20 + \
-            (7.6e-5 if self.dtype == BF16 else 2.7e-6)
+        # matrix unit cuts where it aligns), its product with the scale, the exponential (2^-21)
+        far = torch.einsum("hd,khd->hk", q.double().abs(), k.abs()).amax(1) * abs(scale) * (d + 4) * 2.0 ** -22 + 2.0 ** -20
         out = torch.einsum("hk,khd->hd", p, v)
         sizes = torch.einsum("hk,khd->hd", p, v.abs())
         # fp16: P, at most 2^15, is a multiple of 2^-30 of its largest value or finer below its normal range
