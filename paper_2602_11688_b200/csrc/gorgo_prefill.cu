@@ -11,8 +11,8 @@
 //
 // A block takes one kv head and two tiles of 128 rows, floor(128 / group) tokens each with all their query heads, so
 // that keys and values serve a whole group and both tiles.  Warps: 0-3 and 4-7 softmax of the tiles, a row a thread
-// (TMEM lane), no shuffles; 8 copies; 9 issues tcgen05.mma (10 and 11 only hand in registers), S of one tile while the other is in softmax.  TMEM: S of
-// both tiles (P of 16 bits takes the place of the S it came from, and is the first operand of P V there), O of both.
+// (TMEM lane), no shuffles; 8 copies; 9 issues tcgen05.mma, S of one tile while the other is in softmax; 10 finds the
+// work; 11 clears what lies behind a sequence's last key.  TMEM: S of both tiles (P of 16 bits takes the place of the S it came from, and is the first operand of P V there), O of both.
 // Keys and values come page by page in tiled bulk copies, 128 keys a slot, each as planes of 128-byte rows with
 // the 128-byte swizzle; V is the second operand as it lies (its dims contiguous).
 //
@@ -20,7 +20,10 @@
 // that is not finite and that a row of its tile does not see would reach the row as 0 * x: rows whose result is not
 // finite look at the values behind their own last key, and are computed again key by key if one of those is the cause.
 //
-// Few rows against long prefixes: the keys are split among blocks and joined by a second kernel.
+// All (sequence, kv head, tokens) units with their tiles of keys, and one position more for what a unit costs besides,
+// are laid out as one line that is cut into as many equal pieces as SMs: no batch, no lengths and no long prefix under a few
+// rows leave an SM idle, and a block has at most two units in part, which a second, small kernel joins.  Warp 10 walks
+// the line ahead of the others, so the next unit's copies and first products run under the last one's end.
 //
 // e4m3 pages are first written out in 16 bits (exactly) into the workspace, once for all rows that read them.
 #include "gorgo_rows.cuh"
@@ -34,35 +37,44 @@ constexpr int kThreads = 384;            // three warpgroups: registers can be m
 constexpr int kKeys = 128;                // keys of a tile
 constexpr uint32_t kPlane = kKeys * 128;  // bytes of 128 rows of 128 bytes
 
+constexpr int kEntries = 4;               // units that the roles of a block may be apart
+
 template <int D>
 struct Sizes {
   static constexpr int kPlanes = D / 64;
   static constexpr int kTile = kPlanes * kPlane;               // bytes of 128 rows of Q, K or V
   static constexpr int kSlots = D == 128 ? 5 : 10;
-  static constexpr int kBars = 2 * kSlots + 11;
-  static constexpr int kBytes = 2 * kTile + kSlots * kTile + 8 * kBars + 128;
+  static constexpr int kBars = 2 * kSlots + 2 * kEntries + 13;
+  static constexpr int kBytes = 2 * kTile + kSlots * kTile + 8 * kBars;
   static constexpr int kO = 256;                               // first TMEM column of O; S of tile i begins at 128 i
 };
 
 struct Plan {
   uint32_t tq;                            // tokens of a tile: floor(128 / group)
-  uint32_t splits;
   uint32_t box;                           // keys of one bulk copy
   uint64_t linear;                        // rows of a head in the 16-bit copy of e4m3 pages; 0: the pages themselves
   uint32_t negate;                        // the scale is negative: S takes -Q
   float scale;                            // |scale| * log2(e)
-  float* part_o;                          // [splits][rows][heads][D]
-  float* part_ml;                         // [splits][rows][heads][2]
+  float* part_o;                          // [2 * grid][256][D]
+  float* part_ml;                         // [2 * grid][256][2]
+  struct Split* split;                    // [grid]
 };
 
-struct Work {                             // what a block does
+struct Work {                             // a unit, or a block's part of it
   uint32_t s, h;                          // sequence, kv head
-  int first, n, kv;                       // its first row, new tokens, tokens in all
-  int q0;                                 // first token of the block
+  int first, n, kv;                       // the sequence's first row, new tokens, tokens in all
+  int q0;                                 // first token of the unit
   int tiles[2];                           // tiles of keys of either tile of rows, from 0
   int lo, hi;                             // the block's share of them
-  uint32_t bad;
+  uint32_t slot;                          // where a part goes; kWhole: the result is written
+  uint32_t bad, last;                     // a wrong page or length; nothing comes after the one before
   uint64_t base;                          // first row of the sequence in the 16-bit copy
+};
+constexpr uint32_t kWhole = 0xffffffffu;
+
+struct Split {                            // a unit whose first part a block has: what the second kernel needs
+  Work w;
+  uint32_t parts;                         // 0: none; else blocks that hold parts, this one and those after it
 };
 
 // ------------------------------------------------------------------ tcgen05
@@ -150,61 +162,177 @@ __device__ __forceinline__ int rows_of(const BatchView& b, uint32_t s) {
   return a < 0 || e < a || (uint32_t)e > b.total_new ? 0 : e - a;
 }
 
-// By one warp: the block's sequence and tokens, the last blocks of a sequence first (they see the most keys).
-__device__ bool find_work(const AttnArgs& a, const Plan& p, Work& w, uint32_t lane) {
-  const int step = 2 * p.tq;
-  uint32_t total = 0;
-  uint64_t base = 0;
-  for (uint32_t s = lane; s < a.b.n_seqs; s += 32) total += (rows_of(a.b, s) + step - 1) / step;
-  total = __reduce_add_sync(0xffffffffu, total);
-  if (blockIdx.x >= total) return false;
-  const uint32_t want = total - 1 - blockIdx.x;
-  uint32_t before = 0;
-  for (uint32_t s0 = 0;; s0 += 32) {
-    const uint32_t s = s0 + lane;
-    const int n = s < a.b.n_seqs ? rows_of(a.b, s) : 0;
-    uint32_t mine = (n + step - 1) / step, upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= (uint32_t)d) upto += o;
-    }
-    const uint32_t over = __ballot_sync(0xffffffffu, before + upto > want);
-    const uint32_t here = over ? __ffs(over) - 1 : 32;
-    if (p.linear) {                       // the sequences before it in the 16-bit copy, each from a multiple of 128
-      const int kv = s < a.b.n_seqs && lane < here ? a.b.kv_len[s] : 0;
-      base += __reduce_add_sync(0xffffffffu, kv_len_ok(a.b, kv) ? (uint32_t)(kv + kKeys - 1) / kKeys : 0);
-    }
-    if (over) {
-      w.s = s0 + here;
-      w.n = __shfl_sync(0xffffffffu, n, here);
-      w.q0 = (int)(want - before - __shfl_sync(0xffffffffu, upto - mine, here)) * step;
-      break;
-    }
-    before += __shfl_sync(0xffffffffu, upto, 31);
+// sum of floor((a i + b) / m) over 0 <= i < n, for 0 <= a, b: by the steps of Euclid's algorithm on (a, m).
+__device__ uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+  uint64_t sum = 0;
+  while (n) {
+    sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+    a %= m;
+    b %= m;
+    const uint64_t y = a * n + b;
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const uint64_t t = m;
+    m = a;
+    a = t;
   }
-  w.h = blockIdx.y;
-  w.first = a.b.cu_new[w.s];
-  w.kv = a.b.kv_len[w.s];
-  w.base = base * kKeys;
-  w.bad = !kv_len_ok(a.b, w.kv) || (p.linear && w.base + w.kv > p.linear);
-  if (w.bad) {
-    if (lane == 0) report(a.b.status, GORGO_KV_BAD_LENGTH);
-    w.kv = 0;
-  }
-  int most = 0;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int t = w.q0 + i * (int)p.tq;   // first token of the tile
-    const int last = w.kv - w.n + min(t + (int)p.tq, w.n) - 1;   // position of its last
-    w.tiles[i] = t >= w.n || last < 0 ? 0 : last / kKeys + 1;
-    most = max(most, w.tiles[i]);
-  }
-  const int share = (most + (int)p.splits - 1) / (int)p.splits;
-  w.lo = min(most, (int)blockIdx.z * share);
-  w.hi = min(most, w.lo + share);
-  return true;
+  return sum;
 }
+
+// Tiles of keys of unit q of a sequence with n new tokens of kv: its last token sees the most.
+__device__ __forceinline__ int unit_tiles(int q, int step, int n, int kv) {
+  const int last = kv - n + min((q + 1) * step, n) - 1;
+  return last < 0 ? 0 : last / kKeys + 1;
+}
+// Places on the line before unit q (<= ceil(n / step)) of one kv head: each unit's tiles and one more.
+__device__ uint64_t places_before(int q, int step, int n, int kv) {
+  uint64_t sum = (uint64_t)q;
+  const int units = (n + step - 1) / step;
+  if (q == units && q) {                  // the last unit may be short
+    sum += unit_tiles(q - 1, step, n, kv);
+    --q;
+  }
+  // units i < q: ceil((kv - n + (i + 1) step) / 128), none below zero
+  const int none = kv < n ? (n - kv) / step : 0;               // units whose last token sees nothing
+  if (q > none) sum += floor_sum(q - none, kKeys, step, (uint64_t)(kv - n + (none + 1) * step + kKeys - 1));
+  return sum;
+}
+
+struct SeqPlace {
+  int first, n, kv;
+  bool bad;
+};
+__device__ __forceinline__ SeqPlace seq_place(const AttnArgs& a, uint32_t s) {
+  SeqPlace r = {0, 0, 0, false};
+  if (s >= a.b.n_seqs) return r;
+  r.first = a.b.cu_new[s];
+  r.n = rows_of(a.b, s);
+  r.kv = a.b.kv_len[s];
+  if (!kv_len_ok(a.b, r.kv)) { r.kv = 0; r.bad = true; }       // (its units see no keys, and say NaN)
+  return r;
+}
+
+// Walks a block's piece of the line; all lanes of one warp together.
+struct Walk {
+  uint64_t left;                          // places of the piece from here on
+  uint64_t at;                            // place on the whole line
+  uint64_t total;
+  uint32_t pieces;
+  uint32_t s, h;
+  int q, units;
+  uint64_t off;                           // place inside the unit
+  SeqPlace seq;
+  uint64_t base;                          // tiles of 128 keys of the sequences before
+
+  // False if the block has no piece.
+  __device__ bool begin(const AttnArgs& a, int step, uint32_t lane) {
+    const uint32_t hk = a.kv.n_kv_heads;
+    total = 0;
+    for (uint32_t x = lane; x < a.b.n_seqs; x += 32) {
+      const SeqPlace y = seq_place(a, x);
+      total += places_before((y.n + step - 1) / step, step, y.n, y.kv);
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
+    total *= hk;
+    pieces = total / 4 >= gridDim.x ? gridDim.x : total < 8 ? 1 : (uint32_t)(total / 4);
+    if (blockIdx.x >= pieces || total == 0) return false;
+    at = total * blockIdx.x / pieces;
+    left = total * (blockIdx.x + 1) / pieces - at;
+    uint64_t before = 0;
+    base = 0;
+    for (uint32_t s0 = 0;; s0 += 32) {
+      const SeqPlace y = seq_place(a, s0 + lane);
+      const uint64_t mine = places_before((y.n + step - 1) / step, step, y.n, y.kv) * hk;
+      uint64_t upto = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const uint64_t o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= (uint32_t)d) upto += o;
+      }
+      const uint32_t over = __ballot_sync(0xffffffffu, before + upto > at);
+      const uint32_t here = over ? __ffs(over) - 1 : 32;
+      base += __reduce_add_sync(0xffffffffu, lane < here ? (uint32_t)(y.kv + kKeys - 1) / kKeys : 0);
+      if (over) {
+        s = s0 + here;
+        before += __shfl_sync(0xffffffffu, upto - mine, here);
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    seq = seq_place(a, s);
+    units = (seq.n + step - 1) / step;
+    const uint64_t each = places_before(units, step, seq.n, seq.kv);
+    off = at - before;
+    h = (uint32_t)(off / each);
+    off %= each;
+    // the unit that holds place `off` of the head: 32 candidates at a time
+    int lo = 0, hi = units;                                    // places_before(lo) <= off < places_before(hi)
+    while (hi - lo > 1) {
+      const int gap = (hi - lo + 31) / 32, x = lo + (int)(lane + 1) * gap;
+      const uint32_t c = __popc(__ballot_sync(0xffffffffu, x < hi && places_before(x, step, seq.n, seq.kv) <= off));
+      lo += (int)c * gap;
+      hi = min(hi, lo + gap);
+    }
+    q = lo;
+    off -= places_before(q, step, seq.n, seq.kv);
+    return true;
+  }
+
+  // The next unit or part of one; false at the end of the piece.
+  __device__ bool next(const AttnArgs& a, const Plan& p, int step, Work& w) {
+    while (left) {
+      const int tiles = unit_tiles(q, step, seq.n, seq.kv);
+      const uint64_t take = min(left, (uint64_t)tiles + 1 - off);
+      // place 0 of a unit is what it costs besides; place 1 + i is tile i
+      w.lo = off ? (int)off - 1 : 0;
+      w.hi = (int)(off + take) - 1;
+      const bool some = w.hi > w.lo || tiles == 0;
+      w.s = s;
+      w.h = h;
+      w.first = seq.first;
+      w.n = seq.n;
+      w.kv = seq.kv;
+      w.q0 = q * step;
+      w.base = base * kKeys;
+      w.bad = seq.bad || (p.linear && w.base + seq.kv > p.linear);
+      w.last = 0;
+      for (int i = 0; i < 2; ++i) {
+        const int t = w.q0 + i * (int)p.tq;                    // first token of the tile
+        const int last = seq.kv - seq.n + min(t + (int)p.tq, seq.n) - 1;
+        w.tiles[i] = t >= seq.n || last < 0 ? 0 : last / kKeys + 1;
+      }
+      w.slot = w.lo == 0 && w.hi == tiles ? kWhole : 2 * blockIdx.x + (w.lo == 0 ? 1 : 0);
+      const uint64_t end = at + (uint64_t)tiles + 1 - off;     // of the unit, on the line
+      at += take;
+      left -= take;
+      off += take;
+      if (off == (uint64_t)tiles + 1) {
+        off = 0;
+        if (++q == units) {
+          q = 0;
+          if (++h == a.kv.n_kv_heads) {
+            h = 0;
+            do {
+              base += (uint64_t)(seq.kv + kKeys - 1) / kKeys;
+              seq = seq_place(a, ++s);
+            } while (seq.n == 0 && s < a.b.n_seqs);
+            units = (seq.n + step - 1) / step;
+          }
+        }
+      }
+      if (!some) continue;
+      unit_end = end;
+      return true;
+    }
+    return false;
+  }
+  uint64_t unit_end;                      // of the unit that next() gave
+
+  // Blocks after this one that hold parts of it.
+  __device__ uint32_t blocks_after() const { return (uint32_t)((unit_end * pieces - 1) / total) - blockIdx.x; }
+};
 
 // Waits; on the limit tells the block (and the host) to give up.
 __device__ __forceinline__ bool wait_or_give_up(uint32_t bar, uint32_t parity, volatile uint32_t* quit, uint32_t* status) {
@@ -260,53 +388,49 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
                const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using Z = Sizes<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ Work work;
-  __shared__ uint32_t tmem_base, quit, found;
+  __shared__ Work ring[kEntries];
+  __shared__ uint32_t tmem_base, quit, clear_slot, clear_from;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t q_a = smem_u32(smem), ring_a = q_a + 2 * Z::kTile;
-  const uint32_t bars = ring_a + Z::kSlots * Z::kTile;
-  const uint32_t full = bars, empty = full + 8 * Z::kSlots, q_full = empty + 8 * Z::kSlots, s_full = q_full + 8,
-                 p_full = s_full + 16, o_full = p_full + 32, drained = o_full + 16, tail = drained + 8;
+  const uint32_t full = ring_a + Z::kSlots * Z::kTile, empty = full + 8 * Z::kSlots, work_full = empty + 8 * Z::kSlots,
+                 work_empty = work_full + 8 * kEntries, q_full = work_empty + 8 * kEntries, q_empty = q_full + 8,
+                 s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 32, drained = o_full + 16,
+                 clear = drained + 8, cleared = clear + 8;
 
-  if (warp == 8) {
-    Work w;
-    const bool some = find_work(a, p, w, lane);
-    if (lane == 0) {
-      if (some) work = w;
-      found = some;
-      quit = 0;
-      for (int i = 0; i < Z::kSlots; ++i) {
-        mbar_init(full + 8 * i, 1);
-        mbar_init(empty + 8 * i, 1);
-      }
-      mbar_init(q_full, 1);
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(s_full + 8 * i, 1);
-        mbar_init(p_full + 16 * i, 128);
-        mbar_init(p_full + 16 * i + 8, 128);
-        mbar_init(o_full + 8 * i, 1);
-      }
-      mbar_init(drained, 1);
-      mbar_init(tail, 1);
-      mbar_init_fence();
+  if (threadIdx.x == 0) {
+    quit = 0;
+    for (int i = 0; i < Z::kSlots; ++i) {
+      mbar_init(full + 8 * i, 1);
+      mbar_init(empty + 8 * i, 1);
     }
-  }
-  if (warp == 9 && lane == 0) {
+    for (int i = 0; i < kEntries; ++i) {
+      mbar_init(work_full + 8 * i, 1);
+      mbar_init(work_empty + 8 * i, 10);                       // copies, products, eight warps of softmax
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_full + 16 * i, 128);
+      mbar_init(p_full + 16 * i + 8, 128);
+      mbar_init(o_full + 8 * i, 1);
+    }
+    mbar_init(drained, 1);
+    mbar_init(clear, 1);
+    mbar_init(cleared, 1);
+    mbar_init_fence();
     prefetch_map(&q_map);
     prefetch_map(&k_map);
     prefetch_map(&v_map);
   }
-  __syncthreads();
-  if (!found) return;
   if (warp == 9) tmem_alloc(smem_u32(&tmem_base), 512);
+  launch_dependents();
   fence_before();
   __syncthreads();
   fence_after();
-  const Work w = work;
   const uint32_t tmem = tmem_base;
-  const int steps[2] = {max(0, min(w.hi, w.tiles[0]) - w.lo), max(0, min(w.hi, w.tiles[1]) - w.lo)};
-  const int most = max(steps[0], steps[1]);
-  const bool ragged = most > 0 && (w.lo + most) * kKeys > w.kv;  // the last tile of keys is not full
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_or_give_up(bar, parity, &quit, a.b.status); };
+  auto steps_of = [](const Work& w, int i) { return max(0, min(w.hi, w.tiles[i]) - w.lo); };
 
   // Registers: 384 threads of 168 at the launch; the softmax takes what the last warpgroup does not need
   // (2 * 200 + 104 = 3 * 168).
@@ -316,181 +440,184 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
     const int i = warp / 4;
     const uint32_t r = warp % 4 * 32 + lane, at = tmem + (warp % 4 * 32 << 16);
     const uint32_t s_at = at + 128 * i, o_at = at + Z::kO + D * i;
-    const uint32_t tok = r / a.group;
-    const int t = w.q0 + i * (int)p.tq + (int)tok;             // token of the row
-    const bool mine = tok < p.tq && t < w.n;
-    const int pos = w.kv - w.n + t;
+    const uint32_t tok = r / a.group, in_group = r % a.group;
     const float c = p.scale, slack = 8.f / c;
-    float m = -INFINITY, l = 0.f;
+    uint32_t s_phase = 0, o_phase = 0;
     bool go = true;
-    for (int j = 0; j < steps[i]; ++j) {
-      go = __all_sync(0xffffffffu, wait_or_give_up(s_full + 8 * i, j & 1, &quit, a.b.status));
-      if (!go) break;
-      fence_after();
-      const int seen = pos - (w.lo + j) * kKeys + 1;           // columns that the row sees
-      const bool masked = __any_sync(0xffffffffu, seen < kKeys);
-      // Half of a row at a time: the second half is read twice, which costs less than the registers for all of it.
-      uint32_t x[64];
-      auto read = [&](int k) {
-        tmem_ld32(x, s_at + 64 * k);
-        tmem_ld32(x + 32, s_at + 64 * k + 32);
-        tmem_wait_ld();
-        if (masked) {
-          const int left = seen - 64 * k;
+    for (uint32_t e = 0, e_phase = 0; go; e = (e + 1) % kEntries, e_phase ^= e == 0) {
+      go = __all_sync(0xffffffffu, wait(work_full + 8 * e, e_phase));
+      if (!go || ring[e].last) break;
+      const Work& w = ring[e];
+      const int steps = steps_of(w, i), lo = w.lo;
+      const int t = w.q0 + i * (int)p.tq + (int)tok;           // token of the row
+      const bool mine = tok < p.tq && t < w.n;
+      const int pos = w.kv - w.n + t;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < steps; ++j) {
+        go = __all_sync(0xffffffffu, wait(s_full + 8 * i, s_phase));
+        if (!go) break;
+        s_phase ^= 1;
+        fence_after();
+        const int seen = pos - (lo + j) * kKeys + 1;           // columns that the row sees
+        const bool masked = __any_sync(0xffffffffu, seen < kKeys);
+        // Half of a row at a time: the second half is read twice, which costs less than the registers for all of it.
+        uint32_t x[64];
+        auto read = [&](int k) {
+          tmem_ld32(x, s_at + 64 * k);
+          tmem_ld32(x + 32, s_at + 64 * k + 32);
+          tmem_wait_ld();
+          if (masked) {
+            const int left = seen - 64 * k;
 #pragma unroll
-          for (int y = 0; y < 64; ++y)
-            if (y >= left) x[y] = 0xff800000u;
+            for (int y = 0; y < 64; ++y)
+              if (y >= left) x[y] = 0xff800000u;
+          }
+        };
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int k = 1; k >= 0; --k) {
+          read(k);
+#pragma unroll
+          for (int y = 0; y < 64; y += 2) top[y / 2 % 4] = max3(top[y / 2 % 4], __uint_as_float(x[y]), __uint_as_float(x[y + 1]));
         }
-      };
-      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float now = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
+        const bool grow = !(now <= m + slack);                 // (also for NaN)
+        if (__any_sync(0xffffffffu, grow)) {
+          if (now == INFINITY) now = NAN;                      // infinity - infinity: the row is NaN
+          const float f = grow ? fast_exp2((m - now) * c) : 1.f;
+          if (grow) m = now;
+          l *= f;
+          if (j > 0) {
 #pragma unroll
-      for (int k = 1; k >= 0; --k) {
-        read(k);
+            for (int k = 0; k < D / 32; ++k) {
+              uint32_t o[32];
+              tmem_ld32(o, o_at + 32 * k);
+              tmem_wait_ld();
 #pragma unroll
-        for (int y = 0; y < 64; y += 2) top[y / 2 % 4] = max3(top[y / 2 % 4], __uint_as_float(x[y]), __uint_as_float(x[y + 1]));
-      }
-      float now = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
-      const bool grow = !(now <= m + slack);                   // (also for NaN)
-      if (__any_sync(0xffffffffu, grow)) {
-        if (now == INFINITY) now = NAN;                        // infinity - infinity: the row is NaN
-        const float f = grow ? fast_exp2((m - now) * c) : 1.f;
-        if (grow) m = now;
-        l *= f;
-        if (j > 0) {
-#pragma unroll
-          for (int k = 0; k < D / 32; ++k) {
-            uint32_t o[32];
-            tmem_ld32(o, o_at + 32 * k);
-            tmem_wait_ld();
-#pragma unroll
-            for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
-            tmem_st32(o_at + 32 * k, o);
+              for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+              tmem_st32(o_at + 32 * k, o);
+            }
           }
         }
-      }
-      const float off = m == -INFINITY ? 0.f : kShift<T> - m * c;
-      // P in halves of 64 keys: their products with V begin while the other half is computed
-      f32x2 sum[4] = {0, 0, 0, 0};
-      const f32x2 c2 = both(c, c), off2 = both(off, off);
+        const float off = m == -INFINITY ? 0.f : kShift<T> - m * c;
+        // P in halves of 64 keys: their products with V begin while the other half is computed
+        f32x2 sum[4] = {0, 0, 0, 0};
+        const f32x2 c2 = both(c, c), off2 = both(off, off);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (k) read(1);
+        for (int k = 0; k < 2; ++k) {
+          if (k) read(1);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint32_t pk[16];
+          for (int q = 0; q < 2; ++q) {
+            uint32_t pk[16];
 #pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            float2 e = apart(fma2(both(__uint_as_float(x[32 * q + 2 * y]), __uint_as_float(x[32 * q + 2 * y + 1])), c2, off2));
-            e.x = fast_exp2(e.x);
-            e.y = fast_exp2(e.y);
-            sum[y % 4] = add2(sum[y % 4], both(e.x, e.y));
-            pk[y] = pack2(e.x, e.y, T());
+            for (int y = 0; y < 16; ++y) {
+              float2 u = apart(fma2(both(__uint_as_float(x[32 * q + 2 * y]), __uint_as_float(x[32 * q + 2 * y + 1])), c2, off2));
+              u.x = fast_exp2(u.x);
+              u.y = fast_exp2(u.y);
+              sum[y % 4] = add2(sum[y % 4], both(u.x, u.y));
+              pk[y] = pack2(u.x, u.y, T());
+            }
+            tmem_st16(s_at + 32 * k + 16 * q, pk);
           }
-          tmem_st16(s_at + 32 * k + 16 * q, pk);
+          tmem_wait_st();
+          fence_before();
+          mbar_arrive(p_full + 8 * (2 * i + k));
         }
-        tmem_wait_st();
-        fence_before();
-        mbar_arrive(p_full + 8 * (2 * i + k));
+        const float2 l2 = apart(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+        l += l2.x + l2.y;
       }
-      const float2 l2 = apart(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
-      l += l2.x + l2.y;
-    }
-    if (steps[i] && go) {
-      go = __all_sync(0xffffffffu, wait_or_give_up(o_full + 8 * i, 0, &quit, a.b.status));
-      fence_after();
-    }
-    const uint32_t head = w.h * a.group + r % a.group;
-    const size_t row = (size_t)(w.first + t);
-    const bool bad = work.bad != 0 || !go;
-    if (p.splits > 1) {
-      const size_t part = ((size_t)blockIdx.z * a.b.total_new + row) * a.n_heads + head;
-      if (mine) *reinterpret_cast<float2*>(p.part_ml + 2 * part) = make_float2(m * c, bad ? NAN : l);
-#pragma unroll
-      for (int k = 0; k < D / 32; ++k) {
-        if (!steps[i] || !go) break;
-        uint32_t o[32];
-        tmem_ld32(o, o_at + 32 * k);
-        tmem_wait_ld();
-        if (mine)
-#pragma unroll
-          for (int y = 0; y < 8; ++y)
-            *reinterpret_cast<uint4*>(p.part_o + part * D + 32 * k + 4 * y) = make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
+      if (steps && go) {
+        go = __all_sync(0xffffffffu, wait(o_full + 8 * i, o_phase));
+        o_phase ^= 1;
+        fence_after();
       }
-    } else {
-      // a row without keys: zeros
-      const float inv = bad ? NAN : l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-      bool odd = false;
-      T* out = static_cast<T*>(a.out) + row * a.out_stride + (size_t)head * D;
+      const bool bad = w.bad != 0 || !go;
+      if (w.slot != kWhole) {
+        const size_t part = (size_t)w.slot * 256 + i * 128 + r;
+        *reinterpret_cast<float2*>(p.part_ml + 2 * part) = make_float2(m * c, bad ? NAN : l);
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k) {
-        uint32_t o[32];
-        if (steps[i] && go) {
+        for (int k = 0; k < D / 32; ++k) {
+          if (!steps || !go) break;
+          uint32_t o[32];
           tmem_ld32(o, o_at + 32 * k);
           tmem_wait_ld();
-        } else {
+          if (mine)
 #pragma unroll
-          for (int y = 0; y < 32; ++y) o[y] = 0;
+            for (int y = 0; y < 8; ++y)
+              *reinterpret_cast<uint4*>(p.part_o + part * D + 32 * k + 4 * y) = make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
         }
-        uint4 v[4];
-        uint32_t* u = reinterpret_cast<uint32_t*>(v);
+      } else {
+        const uint32_t head = w.h * a.group + in_group;
+        const size_t row = (size_t)(w.first + t);
+        // a row without keys: zeros
+        const float inv = bad ? NAN : l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+        bool odd = false;
+        T* out = static_cast<T*>(a.out) + row * a.out_stride + (size_t)head * D;
 #pragma unroll
-        for (int y = 0; y < 16; ++y) {
-          const float f = __uint_as_float(o[2 * y]) * inv, g = __uint_as_float(o[2 * y + 1]) * inv;
-          odd |= !(fabsf(f) < INFINITY) || !(fabsf(g) < INFINITY);
-          u[y] = pack2(f, g, T());
+        for (int k = 0; k < D / 32; ++k) {
+          uint32_t o[32];
+          if (steps && go) {
+            tmem_ld32(o, o_at + 32 * k);
+            tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = 0;
+          }
+          uint4 v[4];
+          uint32_t* u = reinterpret_cast<uint32_t*>(v);
+#pragma unroll
+          for (int y = 0; y < 16; ++y) {
+            const float f = __uint_as_float(o[2 * y]) * inv, g = __uint_as_float(o[2 * y + 1]) * inv;
+            odd |= !(fabsf(f) < INFINITY) || !(fabsf(g) < INFINITY);
+            u[y] = pack2(f, g, T());
+          }
+          if (mine)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) *reinterpret_cast<uint4*>(out + 32 * k + 8 * y) = v[y];
         }
-        if (mine)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) *reinterpret_cast<uint4*>(out + 32 * k + 8 * y) = v[y];
+        if (mine && a.lse) a.lse[row * a.n_heads + head] = bad ? NAN : l == 0.f ? -INFINITY : (m * c - kShift<T> + log2f(l)) * 0.693147180559945309f;
+        uint32_t again = __ballot_sync(0xffffffffu, mine && odd && !bad);
+        for (; again; again &= again - 1) {
+          const uint32_t b = __ffs(again) - 1;
+          mend_row<T, D>(a, w.s, __shfl_sync(0xffffffffu, pos, b), w.tiles[i] * kKeys, w.kv, (uint32_t)__shfl_sync(0xffffffffu, (int)row, b),
+                         __shfl_sync(0xffffffffu, head, b), lane);
+        }
       }
-      if (mine && a.lse) a.lse[row * a.n_heads + head] = bad ? NAN : l == 0.f ? -INFINITY : (m * c - kShift<T> + log2f(l)) * 0.693147180559945309f;
-      uint32_t again = __ballot_sync(0xffffffffu, mine && odd && !bad);
-      for (; again; again &= again - 1) {
-        const uint32_t b = __ffs(again) - 1;
-        mend_row<T, D>(a, w.s, __shfl_sync(0xffffffffu, pos, b), w.tiles[i] * kKeys, w.kv, (uint32_t)__shfl_sync(0xffffffffu, (int)row, b),
-                       __shfl_sync(0xffffffffu, head, b), lane);
-      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(work_empty + 8 * e);
     }
-    fence_before();
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 8) {
-      // ---------------------------------------------------------------- copies
-      if (most > 0) {
-        if (lane == 0) {
-          const uint32_t rows = p.tq * a.group;
-          uint32_t bytes = 0;
-          for (int i = 0; i < 2; ++i) bytes += steps[i] ? Z::kPlanes * rows * 128 : 0;
-          mbar_expect(q_full, bytes);
-          for (int i = 0; i < 2; ++i)
-            for (int c = 0; steps[i] && c < Z::kPlanes; ++c)
-              asm volatile(
-                  "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                  ::"r"(q_a + i * Z::kTile + c * kPlane), "l"(reinterpret_cast<uint64_t>(&q_map)), "r"(c * 64),
-                  "r"((int)(w.h * a.group)), "r"(w.first + w.q0 + i * (int)p.tq), "r"(q_full) : "memory");
-        }
+      // -------------------------------------------------------------- copies
+      const uint32_t most_pieces = kKeys / p.box;
+      uint32_t slot = 0, phase = 1, copied = 0, q_phase = 1;
+      bool go = true;
+      for (uint32_t e = 0, e_phase = 0; go; e = (e + 1) % kEntries, e_phase ^= e == 0) {
+        go = __all_sync(0xffffffffu, wait(work_full + 8 * e, e_phase));
+        if (!go || ring[e].last) break;
+        const Work w = ring[e];
+        const int steps[2] = {steps_of(w, 0), steps_of(w, 1)}, most = max(steps[0], steps[1]);
         // a lane a piece: the piece's page is looked up a tile ahead
-        const uint32_t most_pieces = kKeys / p.box;
         auto row_of = [&](int j) -> int64_t {
           const int key = (w.lo + j) * kKeys + (int)(lane * p.box);
-          if (lane >= most_pieces || key >= w.kv) return -2;
-          if (p.linear) return (int64_t)(w.h * p.linear + w.base + key);
+          if (j >= most || lane >= most_pieces || key >= w.kv) return -2;
+          if (p.linear) return w.bad ? 0 : (int64_t)(w.h * p.linear + w.base + key);
           return pool_row(a.kv, a.b, w.s, w.h, (uint32_t)key);
         };
         int64_t row = row_of(0);
-        uint32_t slot = 0, phase = 1, copied = 0;
-        bool go = true;
         for (int j = 0; go && j < most; ++j) {
-          if (row == -1) {                  // a wrong page: copies something that is there, and says so
+          if (row == -1) {                // a wrong page: copies something that is there, and says so
             report(a.b.status, GORGO_KV_BAD_PAGE);
-            work.bad = 1;
+            ring[e].bad = 1;
             row = 0;
           }
           const uint32_t pieces = __popc(__ballot_sync(0xffffffffu, row >= 0));
-          const int64_t next = j + 1 < most ? row_of(j + 1) : -2;
+          const int64_t next = row_of(j + 1);
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
-            go = __all_sync(0xffffffffu, wait_or_give_up(empty + 8 * slot, phase, &quit, a.b.status));
+            go = __all_sync(0xffffffffu, wait(empty + 8 * slot, phase));
             if (!go) break;
             if (lane == 0) mbar_expect(full + 8 * slot, pieces * p.box * D * 2);
             __syncwarp();
@@ -501,29 +628,34 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
             if (++slot == (uint32_t)Z::kSlots) { slot = 0; phase ^= 1; }
           }
           row = next;
-        }
-        if (ragged && go) {                 // what lies behind the last key becomes zeros
-          const uint32_t last = copied - 1, at = last % Z::kSlots;
-          if (__all_sync(0xffffffffu, wait_or_give_up(full + 8 * at, last / Z::kSlots & 1, &quit, a.b.status))) {
-            const uint32_t here = w.kv - (w.lo + most - 1) * kKeys, rest = (kKeys - here) * 8;
-            for (uint32_t x = lane; x < rest * Z::kPlanes; x += 32)
-              *reinterpret_cast<uint4*>(smem + 2 * Z::kTile + at * Z::kTile + x / rest * kPlane + here * 128 + x % rest * 16) =
-                  make_uint4(0, 0, 0, 0);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(tail);
+          if (j == 0 && go) {             // Q behind the first keys: its place is free only after the last unit's scores
+            go = __all_sync(0xffffffffu, wait(q_empty, q_phase));
+            if (!go) break;
+            q_phase ^= 1;
+            if (lane == 0) {
+              const uint32_t bytes = p.tq * a.group * 128 * Z::kPlanes;
+              mbar_expect(q_full, (steps[0] ? bytes : 0) + (steps[1] ? bytes : 0));
+              for (int i = 0; i < 2; ++i)
+                for (int c = 0; steps[i] && c < Z::kPlanes; ++c)
+                  asm volatile(
+                      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                      ::"r"(q_a + i * Z::kTile + c * kPlane), "l"(reinterpret_cast<uint64_t>(&q_map)), "r"(c * 64),
+                      "r"((int)(w.h * a.group)), "r"(w.first + w.q0 + i * (int)p.tq), "r"(q_full) : "memory");
+            }
           }
         }
-        if (quit) {                         // what flies has to land before the block ends
-          mbar_wait(q_full, 0);
-          for (uint32_t i = 0; i < min(copied, (uint32_t)Z::kSlots); ++i)
-            mbar_wait(full + 8 * i, i < slot ? phase ^ 1 : phase);         // the last copy into the slot
-        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(work_empty + 8 * e);
+      }
+      if (quit) {                         // what flies has to land before the block ends
+        mbar_wait(q_full, q_phase);
+        for (uint32_t i = 0; i < min(copied, (uint32_t)Z::kSlots); ++i)
+          mbar_wait(full + 8 * i, i < slot ? phase ^ 1 : phase);         // the last copy into the slot
       }
     } else if (warp == 9) {
       // -------------------------------------------------------------- products: one thread, nothing between two waits
       // but the issue itself (the tensor pipe takes few instructions ahead, so what this thread does besides shows)
-      if (most > 0 && elect_one()) {
+      if (elect_one()) {
         constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
         const uint32_t s_shape = mma_shape(kKeys, kBf, p.negate != 0, false), o_shape = mma_shape(D, kBf, false, true);
         const uint32_t q_op = operand(q_a, 16), k_op = operand(ring_a, 16), v_op = operand(ring_a, kPlane);
@@ -542,51 +674,117 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
           for (int k = 4 * half; k < 4 * half + 4; ++k)
             mma_ts(tmem + Z::kO + D * i, tmem + 128 * i + 8 * k, y + (k * 2048 >> 4), o_shape, acc || k > 0);
         };
-        uint32_t slot = 0, phase = 0;
-        auto take = [&](uint32_t bar) {                        // the next slot, when it is there
-          if (!wait_or_give_up(bar, bar == tail ? 0 : phase, &quit, a.b.status)) return false;
+        uint32_t slot = 0, phase = 0, q_phase = 0, c_phase = 0, p_phase[2] = {0, 0};
+        auto take = [&] {                                      // the next slot, when it is there
+          if (!wait(full + 8 * slot, phase)) return false;
           if (++slot == (uint32_t)Z::kSlots) { slot = 0; phase ^= 1; }
           return true;
         };
-        bool go = wait_or_give_up(q_full, 0, &quit, a.b.status) && take(full);
-        if (go) {
+        bool go = true;
+        for (uint32_t e = 0, e_phase = 0; go; e = (e + 1) % kEntries, e_phase ^= e == 0) {
+          go = wait(work_full + 8 * e, e_phase);
+          if (!go || ring[e].last) break;
+          const int steps[2] = {steps_of(ring[e], 0), steps_of(ring[e], 1)}, most = max(steps[0], steps[1]);
+          const int behind = ring[e].kv - (ring[e].lo + most - 1) * kKeys;   // keys of the last tile
+          mbar_arrive(work_empty + 8 * e);
+          if (most == 0) continue;
+          const uint32_t first_slot = slot;
+          go = take() && wait(q_full, q_phase);
+          q_phase ^= 1;
+          if (!go) break;
           fence_after();
           for (int i = 0; i < 2; ++i)
-            if (steps[i]) scores(i, 0);
-          mma_commit(empty);
-        }
-        for (int j = 0; go && j < most; ++j) {
-          const uint32_t v_slot = slot;
-          if (!take(ragged && j + 1 == most ? tail : full + 8 * slot)) break;
-          uint32_t k_slot = slot;
-          bool have_k = false;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (!go || j >= steps[i]) continue;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              go = go && wait_or_give_up(p_full + 8 * (2 * i + k), j & 1, &quit, a.b.status);
-              fence_after();
-              if (go) values(i, v_slot, k, j > 0);
+            if (steps[i]) scores(i, first_slot);
+          mma_commit(empty + 8 * first_slot);
+          if (most == 1) mma_commit(q_empty);
+          for (int j = 0; go && j < most; ++j) {
+            const uint32_t v_slot = slot;
+            if (!(go = take())) break;
+            if (behind < kKeys && j + 1 == most) {             // what lies behind the last key becomes zeros
+              clear_slot = v_slot;
+              clear_from = behind;
+              mbar_arrive(clear);
+              if (!(go = wait(cleared, c_phase))) break;
+              c_phase ^= 1;
             }
-            if (j + 1 < steps[i]) {
-              if (!have_k) go = go && take(full + 8 * slot);
-              have_k = true;
-              if (go) scores(i, k_slot);
-            } else if (go) {
-              mma_commit(o_full + 8 * i);
+            const uint32_t k_slot = slot;
+            bool have_k = false;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              if (!go || j >= steps[i]) continue;
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                go = go && wait(p_full + 8 * (2 * i + k), p_phase[i]);
+                fence_after();
+                if (go) values(i, v_slot, k, j > 0);
+              }
+              p_phase[i] ^= 1;
+              if (j + 1 < steps[i]) {
+                if (!have_k) go = go && take();
+                have_k = true;
+                if (go) scores(i, k_slot);
+              } else if (go) {
+                mma_commit(o_full + 8 * i);
+              }
             }
+            if (!go) break;
+            mma_commit(empty + 8 * v_slot);
+            if (have_k) mma_commit(empty + 8 * k_slot);
+            if (j + 2 == most) mma_commit(q_empty);
           }
-          if (!go) break;
-          mma_commit(empty + 8 * v_slot);
-          if (have_k) mma_commit(empty + 8 * k_slot);
         }
         if (quit) {                       // products in flight end before the block does
           mma_commit(drained);
           mbar_wait(drained, 0);
         }
+        clear_slot = kWhole;              // (ends warp 11)
+        mbar_arrive(clear);
       }
       __syncwarp();
+    } else if (warp == 10) {
+      // -------------------------------------------------------------- the work, ahead of the others
+      const int step = 2 * (int)p.tq;
+      Walk walk;
+      Work w;
+      uint32_t parts = 0;
+      bool more = walk.begin(a, step, lane), go = true;
+      for (uint32_t e = 0, e_phase = 1; go; e = (e + 1) % kEntries, e_phase ^= e == 0) {
+        more = more && walk.next(a, p, step, w);
+        go = __all_sync(0xffffffffu, wait(work_empty + 8 * e, e_phase));
+        if (lane == 0) {
+          if (more) {
+            ring[e] = w;
+            if (w.bad) report(a.b.status, GORGO_KV_BAD_LENGTH);
+            if (w.slot != kWhole && w.lo == 0) {               // the second kernel finds its parts here and in the blocks behind
+              parts = 1 + walk.blocks_after();
+              p.split[blockIdx.x].w = w;
+            }
+          } else {
+            ring[e].last = 1;
+          }
+          mbar_arrive(work_full + 8 * e);
+        }
+        __syncwarp();
+        if (!more) break;
+      }
+      if (lane == 0) p.split[blockIdx.x].parts = parts;
+    } else {
+      // -------------------------------------------------------------- clears values behind a sequence's last key
+      for (uint32_t c_phase = 0;; c_phase ^= 1) {
+        // (the products' thread always comes to an end and says so; this wait may last as long as all of the work)
+        const long long began = clock64();
+        bool asked;
+        while (!(asked = mbar_try(clear, c_phase)) && clock64() - began < 64 * kWaitTicks) {}
+        if (!__all_sync(0xffffffffu, asked)) break;
+        const uint32_t slot = clear_slot, from = clear_from;
+        if (slot == kWhole) break;
+        const uint32_t rest = (kKeys - from) * 8;              // 16-byte pieces of a plane
+        for (uint32_t x = lane; x < rest * Z::kPlanes; x += 32)
+          *reinterpret_cast<uint4*>(smem + 2 * Z::kTile + slot * Z::kTile + x / rest * kPlane + from * 128 + x % rest * 16) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(cleared);
+      }
     }
   }
   __syncthreads();
@@ -594,47 +792,53 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   if (warp == 9) tmem_free(tmem, 512);
 }
 
-// Joins the parts of one row and head, a warp each.
+// Joins the parts of the units that several blocks hold: a block of this kernel takes 32 rows of the unit whose
+// first part block x of the first kernel has, a warp four of them one after the other.
 template <typename T, int D>
-__global__ void __launch_bounds__(128) prefill_join_kernel(const __grid_constant__ AttnArgs a, const Plan p) {
+__global__ void __launch_bounds__(256) prefill_join_kernel(const __grid_constant__ AttnArgs a, const Plan p) {
   constexpr int kPer = D / 32;
-  const uint32_t lane = threadIdx.x % 32;
-  const uint64_t id = (uint64_t)blockIdx.x * 4 + threadIdx.x / 32;
-  const uint32_t head = (uint32_t)(id % a.n_heads), row = (uint32_t)(id / a.n_heads);
-  if (row >= a.b.total_new) return;
-  const uint32_t s = warp_find_seq(a.b, row, lane);
-  if (s >= a.b.n_seqs) return;
-  const SeqLen q = seq_len(a.b, s);
-  if ((int)row < q.first || rows_of(a.b, s) == 0) return;
-  float top = -INFINITY, sum = 0.f, acc[kPer];
-  const size_t step = (size_t)a.b.total_new * a.n_heads, at = (size_t)row * a.n_heads + head;
-  for (uint32_t i = 0; i < p.splits; ++i) top = fmaxf(top, p.part_ml[2 * (i * step + at)]);
+  const uint32_t lane = threadIdx.x % 32, c0 = blockIdx.x;
+  wait_primary();
+  const uint32_t parts = p.split[c0].parts;
+  if (parts == 0) return;
+  const Work w = p.split[c0].w;
+#pragma unroll 1
+  for (uint32_t r = blockIdx.y * 32 + threadIdx.x / 32; r < blockIdx.y * 32 + 32; r += 8) {
+    const uint32_t i = r / 128, tok = r % 128 / a.group, head = w.h * a.group + r % 128 % a.group;
+    const int t = w.q0 + (int)(i * p.tq + tok);
+    if (tok >= p.tq || t >= w.n) continue;
+    // the first block holds its last unit's part, the others their first one's
+    auto at = [&](uint32_t k) { return (size_t)(2 * (c0 + k) + (k == 0 ? 1 : 0)) * 256 + r; };
+    float top = -INFINITY, sum = 0.f, acc[kPer];
+    for (uint32_t k = lane; k < parts; k += 32) top = fmaxf(top, p.part_ml[2 * at(k)]);
 #pragma unroll
-  for (int y = 0; y < kPer; ++y) acc[y] = 0.f;
-  for (uint32_t i = 0; i < p.splits; ++i) {
-    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * (i * step + at));
-    if (ml.y == 0.f) continue;            // (it has no O)
-    const float f = ml.x == top ? 1.f : fast_exp2(ml.x - top);
-    sum = __fmaf_rn(ml.y, f, sum);
-    const float* o = p.part_o + (i * step + at) * D + lane * kPer;
+    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
 #pragma unroll
-    for (int y = 0; y < kPer; ++y) acc[y] = __fmaf_rn(o[y], f, acc[y]);
-  }
-  const float inv = !q.ok ? NAN : sum == 0.f ? 0.f : 1.f / sum;
-  bool odd = false;
-  T* out = static_cast<T*>(a.out) + (size_t)row * a.out_stride + (size_t)head * D + lane * kPer;
+    for (int y = 0; y < kPer; ++y) acc[y] = 0.f;
+#pragma unroll 4
+    for (uint32_t k = 0; k < parts; ++k) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at(k));
+      if (ml.y == 0.f) continue;          // (it has no O)
+      const float f = ml.x == top ? 1.f : fast_exp2(ml.x - top);
+      sum = __fmaf_rn(ml.y, f, sum);
+      const float* o = p.part_o + at(k) * D + lane * kPer;
 #pragma unroll
-  for (int y = 0; y < kPer; y += 2) {
-    const float f = acc[y] * inv, g = acc[y + 1] * inv;
-    odd |= !(fabsf(f) < INFINITY) || !(fabsf(g) < INFINITY);
-    *reinterpret_cast<uint32_t*>(out + y) = pack2(f, g, T());
-  }
-  if (a.lse && lane == 0) a.lse[at] = !q.ok ? NAN : sum == 0.f ? -INFINITY : (top - kShift<T> + log2f(sum)) * 0.693147180559945309f;
-  if (__any_sync(0xffffffffu, odd) && q.ok && sum == sum) {
-    // keys that the row's tile took: the tile's last token sees the most
-    const int t = (int)row - q.first, pos = q.kv - q.n + t;
-    const int last = q.kv - q.n + min((t / (int)p.tq + 1) * (int)p.tq, q.n) - 1;
-    mend_row<T, D>(a, s, pos, (last / kKeys + 1) * kKeys, q.kv, row, head, lane);
+      for (int y = 0; y < kPer; ++y) acc[y] = __fmaf_rn(o[y], f, acc[y]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    bool odd = false;
+    const size_t row = (size_t)(w.first + t);
+    T* out = static_cast<T*>(a.out) + row * a.out_stride + (size_t)head * D + lane * kPer;
+#pragma unroll
+    for (int y = 0; y < kPer; y += 2) {
+      const float f = acc[y] * inv, g = acc[y + 1] * inv;
+      odd |= !(fabsf(f) < INFINITY) || !(fabsf(g) < INFINITY);
+      *reinterpret_cast<uint32_t*>(out + y) = pack2(f, g, T());
+    }
+    if (a.lse && lane == 0) a.lse[row * a.n_heads + head] = sum == 0.f ? -INFINITY : (top - kShift<T> + log2f(sum)) * 0.693147180559945309f;
+    // (a sum that is NaN: a wrong page, or a score that is none)
+    if (__any_sync(0xffffffffu, odd) && sum == sum)
+      mend_row<T, D>(a, w.s, w.kv - w.n + t, w.tiles[i] * kKeys, w.kv, (uint32_t)row, head, lane);
   }
 }
 
@@ -697,28 +901,19 @@ uint64_t round_up(uint64_t x, uint64_t n) { return (x + n - 1) / n * n; }
 
 struct Layout {
   Plan p;
-  uint32_t blocks;                        // (sequence, tokens) pieces at most
   uint64_t wide, parts, bytes;            // of the 16-bit copy of K (and V), of the parts' O, of all
 };
 
 Layout layout(const AttnArgs& a, int sms) {
   Layout y = {};
   y.p.tq = 128 / a.group;
-  const uint32_t n = a.b.n_seqs < a.b.total_new ? a.b.n_seqs : a.b.total_new;
-  y.blocks = (a.b.total_new - n) / (2 * y.p.tq) + n;           // sum of ceil(n_s / step) is the most when all but one have one token
-  // Keys are split where the blocks would leave half of the SMs idle, in shares of four tiles or more.
-  const uint64_t units = (uint64_t)y.blocks * a.kv.n_kv_heads;
-  uint32_t splits = units * 2 <= (uint64_t)sms ? (uint32_t)(sms / units) : 1;
-  const uint32_t most = (a.b.max_kv + 4 * kKeys - 1) / (4 * kKeys);
-  if (splits > most) splits = most;
-  y.p.splits = splits < 1 ? 1 : splits;
   if (a.store == GORGO_E4M3) {
     y.p.linear = round_up(a.total_kv, kKeys) + (uint64_t)kKeys * a.b.n_seqs;
     y.wide = round_up(y.p.linear * a.kv.n_kv_heads * a.head_dim * 2, 256);
   }
   y.p.box = a.store == GORGO_E4M3 ? kKeys : (1u << a.kv.page_shift) < (uint32_t)kKeys ? 1u << a.kv.page_shift : kKeys;
-  if (y.p.splits > 1) y.parts = round_up((uint64_t)y.p.splits * a.b.total_new * a.n_heads * a.head_dim * 4, 256);
-  y.bytes = 2 * y.wide + y.parts + (y.p.splits > 1 ? (uint64_t)y.p.splits * a.b.total_new * a.n_heads * 8 : 0);
+  y.parts = (uint64_t)2 * sms * 256 * a.head_dim * 4;
+  y.bytes = 2 * y.wide + y.parts + (uint64_t)2 * sms * 256 * 8 + (uint64_t)sms * sizeof(Split);
   return y;
 }
 
@@ -730,6 +925,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   unsigned char* ws = static_cast<unsigned char*>(a.workspace);
   p.part_o = reinterpret_cast<float*>(ws + 2 * y.wide);
   p.part_ml = reinterpret_cast<float*>(ws + 2 * y.wide + y.parts);
+  p.split = reinterpret_cast<Split*>(p.part_ml + (size_t)2 * sms * 256 * 2);
   p.negate = a.scale_log2 < 0.f;
   // (a scale of zero: all scores next to nothing, and what is not seen still at minus infinity)
   p.scale = fmaxf(fabsf(a.scale_log2), 1e-30f);
@@ -750,11 +946,18 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
     return cudaErrorUnknown;
   cudaError_t e = allow_smem<prefill_kernel<T, D>>(Z::kBytes);
   if (e != cudaSuccess) return e;
-  prefill_kernel<T, D><<<dim3(y.blocks, a.kv.n_kv_heads, p.splits), kThreads, Z::kBytes, st>>>(a, p, qm, km, vm);
-  if ((e = cudaGetLastError()) != cudaSuccess || p.splits == 1) return e;
-  const uint64_t warps = (uint64_t)a.b.total_new * a.n_heads;
-  prefill_join_kernel<T, D><<<(uint32_t)((warps + 3) / 4), 128, 0, st>>>(a, p);
-  return cudaGetLastError();
+  prefill_kernel<T, D><<<sms, kThreads, Z::kBytes, st>>>(a, p, qm, km, vm);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(sms, 8);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute early = {};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, prefill_join_kernel<T, D>, a, p);
 }
 
 }  // namespace

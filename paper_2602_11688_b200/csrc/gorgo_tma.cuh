@@ -52,8 +52,9 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// Clock ticks after which a wait gives up: about two seconds, a thousand times what any copy or tile takes.
-constexpr long long kWaitTicks = 4000000000ll;
+// Clock ticks after which a wait gives up: about ten seconds, many times what a unit of work takes, rows that are
+// computed again among it.
+constexpr long long kWaitTicks = 20000000000ll;
 static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
   const long long from = clock64();
   while (!mbar_try(bar, parity))
