@@ -20,8 +20,8 @@
 // that is not finite and that a row of its tile does not see would reach the row as 0 * x: rows whose result is not
 // finite look at the values behind their own last key, and are computed again key by key if one of those is the cause.
 //
-// All (sequence, kv head, tokens) units with their tiles of keys, and one position more for what a unit costs besides,
-// are laid out as one line that is cut into as many equal pieces as SMs: no batch, no lengths and no long prefix under a few
+// All (sequence, kv head, tokens) units with their tiles of keys, and two places more for what a unit costs besides, are
+// laid out as one line that is cut into as many equal pieces as SMs: no batch, no lengths and no long prefix under a few
 // rows leave an SM idle, and a block has at most two units in part, which a second, small kernel joins.  Warp 10 walks
 // the line ahead of the others, so the next unit's copies and first products run under the last one's end.
 //
@@ -38,6 +38,8 @@ constexpr int kKeys = 128;                // keys of a tile
 constexpr uint32_t kPlane = kKeys * 128;  // bytes of 128 rows of 128 bytes
 
 constexpr int kEntries = 4;               // units that the roles of a block may be apart
+constexpr int kUnit = 2;                  // what a unit costs besides its tiles, in tiles (with 1: 747 instead of 894 TFLOP/s on
+                                          // sixteen prompts of about 1,000 tokens; with 3 and 4: 890 and 878)
 
 template <int D>
 struct Sizes {
@@ -185,9 +187,9 @@ __device__ __forceinline__ int unit_tiles(int q, int step, int n, int kv) {
   const int last = kv - n + min((q + 1) * step, n) - 1;
   return last < 0 ? 0 : last / kKeys + 1;
 }
-// Places on the line before unit q (<= ceil(n / step)) of one kv head: each unit's tiles and one more.
+// Places on the line before unit q (<= ceil(n / step)) of one kv head: each unit's tiles and kUnit more.
 __device__ uint64_t places_before(int q, int step, int n, int kv) {
-  uint64_t sum = (uint64_t)q;
+  uint64_t sum = (uint64_t)q * kUnit;
   const int units = (n + step - 1) / step;
   if (q == units && q) {                  // the last unit may be short
     sum += unit_tiles(q - 1, step, n, kv);
@@ -284,11 +286,11 @@ struct Walk {
   __device__ bool next(const AttnArgs& a, const Plan& p, int step, Work& w) {
     while (left) {
       const int tiles = unit_tiles(q, step, seq.n, seq.kv);
-      const uint64_t take = min(left, (uint64_t)tiles + 1 - off);
-      // place 0 of a unit is what it costs besides; place 1 + i is tile i
-      w.lo = off ? (int)off - 1 : 0;
-      w.hi = (int)(off + take) - 1;
-      const bool some = w.hi > w.lo || tiles == 0;
+      const uint64_t take = min(left, (uint64_t)tiles + kUnit - off);
+      // the first places of a unit are what it costs besides; place kUnit + i is tile i
+      w.lo = max(0, (int)off - kUnit);
+      w.hi = max(0, (int)(off + take) - kUnit);
+      const bool some = w.hi > w.lo || (tiles == 0 && off == 0);
       w.s = s;
       w.h = h;
       w.first = seq.first;
@@ -304,11 +306,11 @@ struct Walk {
         w.tiles[i] = t >= seq.n || last < 0 ? 0 : last / kKeys + 1;
       }
       w.slot = w.lo == 0 && w.hi == tiles ? kWhole : 2 * blockIdx.x + (w.lo == 0 ? 1 : 0);
-      const uint64_t end = at + (uint64_t)tiles + 1 - off;     // of the unit, on the line
+      const uint64_t end = at + (uint64_t)tiles + kUnit - off;     // of the unit, on the line
       at += take;
       left -= take;
       off += take;
-      if (off == (uint64_t)tiles + 1) {
+      if (off == (uint64_t)tiles + kUnit) {
         off = 0;
         if (++q == units) {
           q = 0;
@@ -655,7 +657,9 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
     } else if (warp == 9) {
       // -------------------------------------------------------------- products: one thread, nothing between two waits
       // but the issue itself (the tensor pipe takes few instructions ahead, so what this thread does besides shows)
-      if (elect_one()) {
+      // At D = 64 the exponentials are the bound and a thread that issues a little later serves them better: the tiles
+      // fall into turns (20,000 tokens: 733 against 694 TFLOP/s; at D = 128 it is 1,240 against 1,306).
+      if (D == 64 ? lane == 0 : elect_one()) {
         constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
         const uint32_t s_shape = mma_shape(kKeys, kBf, p.negate != 0, false), o_shape = mma_shape(D, kBf, false, true);
         const uint32_t q_op = operand(q_a, 16), k_op = operand(ring_a, 16), v_op = operand(ring_a, kPlane);
