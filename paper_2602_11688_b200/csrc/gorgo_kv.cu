@@ -2,8 +2,8 @@
 //
 // Both move each byte once and compute next to nothing, so the bound is HBM: 2 * T * n_kv_heads * head_dim *
 // (2 + stored bytes) bytes for T tokens, and for a handful of tokens the launch and the chain
-// cu_new -> table -> row.  A block takes a few tokens with all their heads: one warp per token finds the sequence, the
-// page and the slot while the rows are already being loaded; 16 bytes a lane.
+// cu_new -> table -> row.  A block takes a few tokens with all their heads: one warp finds the sequences, pages and slots
+// while the rows are already being loaded; 16 bytes a lane.
 #include "gorgo_attn.cuh"
 
 namespace gorgo {
@@ -11,20 +11,20 @@ namespace gorgo {
 namespace {
 
 constexpr int kMoveThreads = 256;
-constexpr int kMaxTok = 8;                // tokens of a block: one warp finds each one's place
+constexpr int kMaxTok = 32;               // tokens of a block at most: a lane finds each one's place
 
-struct Place {
-  int64_t row;                            // pool row of kv head 0, -1: none
-};
-
-// Warp w of the block finds where token first + w lies.
+// By the first warp: where the tokens first, first + 1, ... lie: the pool row of their kv head 0; -1: the token belongs to no
+// sequence; -2: to one, but has no place.
 __device__ __forceinline__ void find_places(const KvView& kv, const BatchView& b, uint32_t first, uint32_t n_tok,
                                             int64_t* place) {
-  const uint32_t w = threadIdx.x / 32, lane = threadIdx.x % 32;
-  if (w >= n_tok) return;
-  const uint32_t t = first + w;
-  const uint32_t s = warp_find_seq(b, t, lane);
-  if (lane) return;
+  if (threadIdx.x >= 32) return;
+  const uint32_t lane = threadIdx.x, t = first + lane;
+  uint32_t s = warp_find_seq(b, first, lane);
+  if (lane >= n_tok) return;
+  for (; s < b.n_seqs; ++s) {             // neighbours: their sequences are near (and a decreasing cu_new is reported below)
+    const int e = b.cu_new[s + 1];
+    if (e > (int)t || e < b.cu_new[s]) break;
+  }
   int64_t row = -1;
   if (s < b.n_seqs) {                     // (rows behind the last sequence belong to nobody)
     const SeqLen q = seq_len(b, s);
@@ -34,126 +34,187 @@ __device__ __forceinline__ void find_places(const KvView& kv, const BatchView& b
       row = pool_row(kv, b, s, 0, (uint32_t)j);
       if (row < 0) report(b.status, GORGO_KV_BAD_PAGE);
     }
-    if (row < 0) row = -2;                // a token of a sequence, with no place
+    if (row < 0) row = -2;
   }
-  place[w] = row;
+  place[lane] = row;
 }
 
-// One row of a token and kv head belongs to D / 8 lanes, 8 elements each.
+// The larger of two values in each half; NaN if one is.
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b, __nv_bfloat16) {
+  uint32_t y;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b, __half) {
+  uint32_t y;
+  asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
+
+// One row of a token and kv head belongs to D / 8 lanes, 8 elements each; a thread has kAhead rows of K and of V in
+// flight.  The powers of two of neighbouring tokens lie side by side: they are gathered and go out together.
+constexpr int kAhead = 2;
+
 template <typename T, bool kQuant, int D>
 __global__ void __launch_bounds__(kMoveThreads) kv_write_kernel(const KvMoveArgs a, const uint32_t n_tok) {
-  constexpr uint32_t kLanes = D / 8;
+  constexpr uint32_t kLanes = D / 8, kRows = kMoveThreads / kLanes;
+  extern __shared__ int8_t gathered[];                         // [2][heads][n_tok], quantised only
   __shared__ int64_t place[kMaxTok];
   const uint32_t first = blockIdx.x * n_tok;
   const uint32_t here = min(n_tok, a.b.total_new - first), hk = a.kv.n_kv_heads;
-  const uint32_t l = threadIdx.x % kLanes;
-  const uint32_t rows = here * hk;
+  const uint32_t l = threadIdx.x % kLanes, rows = here * hk;
   bool known = false;
-  // the lanes of a row have the same rows, and a warp runs as long as any of its lanes has one
-  for (uint32_t r0 = threadIdx.x / kLanes; r0 - (threadIdx.x % 32) / kLanes < rows || !known; r0 += kMoveThreads / kLanes) {
-    const bool mine = r0 < rows;
-    const uint32_t tok = mine ? r0 / hk : 0, h = mine ? r0 - tok * hk : 0;
-    uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    if (mine) {
+  // a warp runs as long as any of its lanes has a row: lanes of a row take part in its maximum together
+  for (uint32_t r0 = threadIdx.x / kLanes; r0 - (threadIdx.x % 32) / kLanes < rows || !known; r0 += kAhead * kRows) {
+    uint4 x[kAhead][2];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      const uint32_t r = r0 + n * kRows, tok = (uint32_t)(r * a.per_head >> 32), h = r - tok * hk;
+      x[n][0] = x[n][1] = make_uint4(0, 0, 0, 0);
+      if (r >= rows) continue;
       const size_t col = (size_t)h * D + l * 8;
-      x[0] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_in) + (size_t)(first + tok) * a.k_stride + col));
-      x[1] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_in) + (size_t)(first + tok) * a.v_stride + col));
+      x[n][0] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_in) + (size_t)(first + tok) * a.k_stride + col));
+      x[n][1] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_in) + (size_t)(first + tok) * a.v_stride + col));
     }
     if (!known) {
       find_places(a.kv, a.b, first, here, place);
       __syncthreads();
       known = true;
     }
-    const int64_t base = mine ? place[tok] : -1;
-    const int64_t row = base + ((int64_t)h << a.kv.page_shift);
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      void* pool = w ? a.kv.v : a.kv.k;
-      if (!kQuant) {
-        if (base >= 0) *reinterpret_cast<uint4*>(static_cast<T*>(pool) + row * D + l * 8) = x[w];
-        continue;
+    for (int n = 0; n < kAhead; ++n) {
+      const uint32_t r = r0 + n * kRows, tok = (uint32_t)(r * a.per_head >> 32), h = r - tok * hk;
+      const int64_t base = r < rows ? place[tok] : -1;
+      const int64_t row = base + ((int64_t)h << a.kv.page_shift);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        void* pool = w ? a.kv.v : a.kv.k;
+        if (!kQuant) {
+          if (base >= 0) *reinterpret_cast<uint4*>(static_cast<T*>(pool) + row * D + l * 8) = x[n][w];
+          continue;
+        }
+        float f[8];
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(&x[n][w]);
+        // max|x|, two at a time
+        uint32_t most = max2(max2(u[0] & 0x7fff7fffu, u[1] & 0x7fff7fffu, T()), max2(u[2] & 0x7fff7fffu, u[3] & 0x7fff7fffu, T()), T());
+#pragma unroll
+        for (uint32_t m = kLanes / 2; m; m /= 2) most = max2(most, __shfl_xor_sync(0xffffffffu, most, m), T());
+        most = max(most & 0xffffu, most >> 16);
+        const uint32_t top = __float_as_uint(unpack2(most, T()).x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 p = unpack2(u[i], T());
+          f[2 * i] = p.x;
+          f[2 * i + 1] = p.y;
+        }
+        if (base < 0) continue;
+        // max|x| = f * 2^x, 1 <= f < 2, and 448 = 1.75 * 2^8: e = x - 8, one more if f > 1.75
+        const int e = max(kExpMin, (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u));
+        const float inv = pow2i(-e);      // exact, and so is x * inv: the code is rounded once
+        uint32_t c[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i] * inv, f[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+          const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i + 2] * inv, f[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+          c[i] = lo | hi << 16;
+        }
+        if (top >= 0x7f800000u) c[0] = c[1] = 0x7f7f7f7fu;     // an infinity or NaN: the row is NaN
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + row * D + l * 8) = make_uint2(c[0], c[1]);
+        if (l == 0) gathered[(w * hk + h) * n_tok + tok] = (int8_t)(top >= 0x7f800000u ? 0 : e);
       }
-      float f[8];
-      const uint32_t* u = reinterpret_cast<const uint32_t*>(&x[w]);
-      uint32_t top = 0;                   // |x| as bits: their order is that of the values, infinity and NaN on top
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 p = unpack2(u[i], T());
-        f[2 * i] = p.x;
-        f[2 * i + 1] = p.y;
-        top = max(top, max(__float_as_uint(p.x) & 0x7fffffffu, __float_as_uint(p.y) & 0x7fffffffu));
+    }
+  }
+  if (!kQuant) return;
+  __syncthreads();
+  for (uint32_t t0 = 0; t0 < here; t0 += 8) {                  // eight neighbours of a page are one store
+    bool side = t0 + 8 <= here && place[t0] >= 0 && place[t0] % 8 == 0;
+    for (uint32_t t = 1; side && t < 8; ++t) side = place[t0 + t] == place[t0] + t;
+    for (uint32_t y = threadIdx.x; y < 2 * hk; y += kMoveThreads) {
+      int8_t* out = (y >= hk ? a.kv.v_exp : a.kv.k_exp) + ((int64_t)(y >= hk ? y - hk : y) << a.kv.page_shift);
+      const int8_t* in = gathered + y * n_tok + t0;
+      if (side) {
+        *reinterpret_cast<uint2*>(out + place[t0]) = *reinterpret_cast<const uint2*>(in);
+      } else {
+        for (uint32_t t = 0; t < min(8u, here - t0); ++t)
+          if (place[t0 + t] >= 0) out[place[t0 + t]] = in[t];
       }
-#pragma unroll
-      for (uint32_t m = kLanes / 2; m; m /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
-      if (base < 0) continue;
-      // max|x| = f * 2^x, 1 <= f < 2, and 448 = 1.75 * 2^8: e = x - 8, one more if f > 1.75
-      const int e = max(kExpMin, (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u));
-      const float inv = pow2i(-e);        // exact, and so is x * inv: the code is rounded once
-      uint32_t c[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i] * inv, f[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i + 2] * inv, f[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-        c[i] = lo | hi << 16;
-      }
-      if (top >= 0x7f800000u) c[0] = c[1] = 0x7f7f7f7fu;   // an infinity or NaN: the row is NaN
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + row * D + l * 8) = make_uint2(c[0], c[1]);
-      if (l == 0) (w ? a.kv.v_exp : a.kv.k_exp)[row] = (int8_t)(top >= 0x7f800000u ? 0 : e);
     }
   }
 }
 
 template <typename T, bool kQuant, int D>
 __global__ void __launch_bounds__(kMoveThreads) kv_read_kernel(const KvMoveArgs a, const uint32_t n_tok) {
-  constexpr uint32_t kLanes = D / 8;
+  constexpr uint32_t kLanes = D / 8, kRows = kMoveThreads / kLanes;
   __shared__ int64_t place[kMaxTok];
   const uint32_t first = blockIdx.x * n_tok;
   const uint32_t here = min(n_tok, a.b.total_new - first), hk = a.kv.n_kv_heads;
   find_places(a.kv, a.b, first, here, place);
   __syncthreads();
-  const uint32_t l = threadIdx.x % kLanes;
-  for (uint32_t r0 = threadIdx.x / kLanes; r0 < here * hk; r0 += kMoveThreads / kLanes) {
-    const uint32_t tok = r0 / hk, h = r0 - tok * hk;
-    const int64_t base = place[tok];
-    if (base == -1) continue;
-    const int64_t row = base + ((int64_t)h << a.kv.page_shift);
-    const size_t col = (size_t)h * D + l * 8;
+  const uint32_t l = threadIdx.x % kLanes, rows = here * hk;
+  for (uint32_t r0 = threadIdx.x / kLanes; r0 < rows; r0 += kAhead * kRows) {
+    uint4 x[kAhead][2];
+    int e[kAhead][2];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const void* pool = w ? a.kv.v : a.kv.k;
-      uint4 x;
-      if (base < 0) {
-        x = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);   // NaN in either type
-      } else if (!kQuant) {
-        x = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(pool) + row * D + l * 8));
-      } else {
-        const uint2 c = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + row * D + l * 8));
-        const float m = pow2i((w ? a.kv.v_exp : a.kv.k_exp)[row]);
-        uint32_t* u = reinterpret_cast<uint32_t*>(&x);
+    for (int n = 0; n < kAhead; ++n) {
+      const uint32_t r = r0 + n * kRows, tok = (uint32_t)(r * a.per_head >> 32), h = r - tok * hk;
+      const int64_t base = r < rows ? place[tok] : -1;
+      const int64_t row = base + ((int64_t)h << a.kv.page_shift);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 p = unpack_e4m3((i < 2 ? c.x : c.y) >> 16 * (i & 1) & 0xffffu);
-          u[i] = pack2(p.x * m, p.y * m, T());             // (the product is exact up to the type's range)
+      for (int w = 0; w < 2; ++w) {
+        const void* pool = w ? a.kv.v : a.kv.k;
+        e[n][w] = 0;
+        if (base < 0) {
+          x[n][w] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);   // NaN in all of the types
+        } else if (!kQuant) {
+          x[n][w] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const T*>(pool) + row * D + l * 8));
+        } else {
+          const uint2 c = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + row * D + l * 8));
+          x[n][w] = make_uint4(c.x, c.y, 0, 0);
+          e[n][w] = (w ? a.kv.v_exp : a.kv.k_exp)[row];
         }
       }
-      T* out = static_cast<T*>(w ? a.v_out : a.k_out);
-      __stcs(reinterpret_cast<uint4*>(out + (size_t)(first + tok) * (w ? a.v_stride : a.k_stride) + col), x);
+    }
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      const uint32_t r = r0 + n * kRows, tok = (uint32_t)(r * a.per_head >> 32), h = r - tok * hk;
+      const int64_t base = r < rows ? place[tok] : -1;
+      if (base == -1) continue;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        uint4 y = x[n][w];
+        if (kQuant && base >= 0) {
+          const float m = pow2i(e[n][w]);
+          uint32_t* u = reinterpret_cast<uint32_t*>(&y);
+          const uint32_t c[2] = {x[n][w].x, x[n][w].y};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 p = unpack_e4m3(c[i >> 1] >> 16 * (i & 1) & 0xffffu);
+            u[i] = pack2(p.x * m, p.y * m, T());               // (the product is exact up to the type's range)
+          }
+        }
+        T* out = static_cast<T*>(w ? a.v_out : a.k_out);
+        __stcs(reinterpret_cast<uint4*>(out + (size_t)(first + tok) * (w ? a.v_stride : a.k_stride) + (size_t)h * D + l * 8), y);
+      }
     }
   }
 }
 
 template <bool kWrite, typename T, bool kQuant, int D>
 cudaError_t launch_move(const KvMoveArgs& a, cudaStream_t st) {
-  // Few tokens: one a block, so that their chains run side by side; else as many as keep 148 SMs in work.
-  const uint32_t n_tok = a.b.total_new < 8u * 148u ? 1 : kMaxTok;
+  // Few tokens: one a block, so that their chains run side by side.  Many: eight, or 32 where codes are written (128,000
+  // tokens: 154 against 165 us; read, 32 are 360 against 349 us), if the gathered powers of two leave room for them.
+  const uint32_t per = a.b.total_new / (8u * 148u);
+  const uint32_t n_tok = per < 2 ? 1 : per < 32 || !kWrite || !kQuant || a.kv.n_kv_heads > 64 ? 8 : kMaxTok;
   const uint32_t grid = (a.b.total_new + n_tok - 1) / n_tok;
-  if (kWrite) kv_write_kernel<T, kQuant, D><<<grid, kMoveThreads, 0, st>>>(a, n_tok);
+  if (kWrite) kv_write_kernel<T, kQuant, D><<<grid, kMoveThreads, kQuant ? 2 * a.kv.n_kv_heads * n_tok : 0, st>>>(a, n_tok);
   else kv_read_kernel<T, kQuant, D><<<grid, kMoveThreads, 0, st>>>(a, n_tok);
   return cudaGetLastError();
 }
 
 template <bool kWrite>
-cudaError_t dispatch_move(const KvMoveArgs& a, cudaStream_t st) {
+cudaError_t dispatch_move(KvMoveArgs a, cudaStream_t st) {
+  // r / n_kv_heads = r * per_head / 2^32 for r < 2^22: per_head is too large by less than 1
+  a.per_head = ((1ull << 32) + a.kv.n_kv_heads - 1) / a.kv.n_kv_heads;
   const bool q = a.store == GORGO_E4M3, b = a.type == GORGO_BF16, d = a.head_dim == 128;
   if (b) {
     if (q) return d ? launch_move<kWrite, __nv_bfloat16, true, 128>(a, st) : launch_move<kWrite, __nv_bfloat16, true, 64>(a, st);
