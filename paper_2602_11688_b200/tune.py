@@ -6,7 +6,7 @@ policies of Section 4, all replayed through the same simulator.
 
 Prints one JSON line per ES step and a final JSON object with the policy table.  Everything is
 computed by the library (there is no CPU path); numpy only draws the normal perturbations, which
-are an input of the strategy.
+are an input of the strategy.  With ``--engine`` the service model's constants are measured first (``service.py``).
 """
 from __future__ import annotations
 
@@ -28,11 +28,21 @@ def main(argv=None):
     ap.add_argument("--seed", type=int, default=0)
     ap.add_argument("--objective", choices=["ttft", "e2e"], default="ttft")
     ap.add_argument("--scale", type=float, default=None, help="time scale (default: the workload's)")
+    ap.add_argument("--engine", default=None, metavar="LxHxFxNxKxD",
+                    help="measure the service model on this GPU with a decoder of this shape (layers, hidden,\n"
+                         "feed-forward, heads, kv heads, head dim) instead of taking the workload's constants")
+    ap.add_argument("--kv-type", choices=["bf16", "fp16", "e4m3"], default="bf16",
+                    help="with --engine: what the key-value cache holds")
     args = ap.parse_args(argv)
 
     import torch
     from . import binding as gb
+    from . import service as S
     from . import workloads as W
+    try:
+        shape = None if args.engine is None else S.EngineShape.parse(args.engine)
+    except ValueError as e:
+        ap.error(str(e))
 
     kw = {"population": 1}
     if args.requests:
@@ -40,7 +50,20 @@ def main(argv=None):
     w = W.make_workload(args.workload, **kw)
     scale = float(w.spec.time_scales[0]) if args.scale is None else args.scale
     K, R, N = w.n_params, w.spec.n_replicas, w.n_requests
+    measured = None
+    if shape is not None:
+        measured = S.measure(w, shape, args.kv_type)
+        # a replica's cache is never smaller than the longest prompt, else the trace could not be replayed
+        longest = int(np.diff(w.hash_off.astype(np.int64)).max())
+        w.spec.prefill_ms_per_token = measured["prefill_ms_per_token"]
+        w.spec.tpot_ms = measured["tpot_ms"]
+        w.spec.cache_blocks = max(longest, measured["cache_blocks"])
+        print(json.dumps({"service": measured, "kv_type": args.kv_type}))
     sim = gb.GorgoSim(w)
+    if measured is not None:
+        rc = gb.gorgo_sim_set_service_model(sim.h, measured["decode_slowdown"], measured["kv_budget_tokens"])
+        if rc != gb.GORGO_OK:
+            raise gb.GorgoError(rc, "gorgo_sim_set_service_model")
     dev = sim.device
     sim.ensure_workspace(max(args.lam, 1), max_bytes=int(torch.cuda.mem_get_info(dev)[0] * 0.8))
 
