@@ -497,8 +497,8 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
 }
 
 // Joins what several blocks hold of one query head, and answers for sequences without keys.  A block a head: its
-// threads take every fourth or eighth part, 16 bytes of the row each, so that parts arrive side by side.
-constexpr int kJoinThreads = 128;
+// threads take every 8th or 16th part, 16 bytes of the row each, with a running maximum, so that parts arrive side by side.
+constexpr int kJoinThreads = 256;
 template <typename T, int kTile, int D, int NB>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArgs a, const Split sp) {
   constexpr uint32_t kH = 8 * NB, kVec = D / 4, kWays = kJoinThreads / kVec;
@@ -506,8 +506,9 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArg
   if (h >= a.group - hh % sp.ng * kH) { wait_primary(); return; }
   const uint32_t head = hh / sp.ng * a.group + hh % sp.ng * kH + h;
   const uint32_t way = threadIdx.x / kVec, d = threadIdx.x % kVec * 4;
-  __shared__ unsigned long long sums[2][4];
-  __shared__ float red[4], part[kWays][D + 1];
+  constexpr uint32_t kJoinWarps = kJoinThreads / 32;
+  __shared__ unsigned long long sums[2][kJoinWarps];
+  __shared__ float part[kWays][D + 4];
   uint64_t before = 0, total = 0;
   for (uint32_t x = threadIdx.x; x < a.b.n_seqs; x += kJoinThreads) {
     const uint32_t n = tiles_of<kTile>(a.b, x);
@@ -521,8 +522,13 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArg
   }
   if (threadIdx.x % 32 == 0) { sums[0][threadIdx.x / 32] = before; sums[1][threadIdx.x / 32] = total; }
   __syncthreads();
-  before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-  total = (sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3]) * sp.hh;
+  before = total = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kJoinWarps; ++i) {
+    before += sums[0][i];
+    total += sums[1][i];
+  }
+  total *= sp.hh;
   const uint32_t nt = tiles_of<kTile>(a.b, s);
   const uint32_t n = pieces(total, sp.grid);
   T* out = static_cast<T*>(a.out) + (size_t)s * a.out_stride + (size_t)head * D + d;
@@ -541,43 +547,39 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArg
   if (c0 == c1) return;
   // the first block holds its last piece of line, the others their first
   auto at = [&](uint32_t c) { return (size_t)(2 * c + (c == c0 ? 1 : 0)) * kH + h; };
-  float top = -INFINITY;
-  for (uint32_t c = c0 + threadIdx.x; c <= c1; c += kJoinThreads) top = fmaxf(top, sp.part_ml[at(c) * 2]);
-#pragma unroll
-  for (int i = 16; i; i /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  float sum = 0.f;
+  float top = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
   for (uint32_t c = c0 + way; c <= c1; c += kWays) {
     const float2 p = *reinterpret_cast<const float2*>(sp.part_ml + at(c) * 2);
     const float4 y = *reinterpret_cast<const float4*>(sp.part_o + at(c) * D + d);
-    const float w = p.x == top ? 1.f : fast_exp2(p.x - top);
-    sum = __fmaf_rn(p.y, w, sum);
-    acc.x = __fmaf_rn(y.x, w, acc.x);
-    acc.y = __fmaf_rn(y.y, w, acc.y);
-    acc.z = __fmaf_rn(y.z, w, acc.z);
-    acc.w = __fmaf_rn(y.w, w, acc.w);
+    const float now = fmaxf(top, p.x);
+    const float f = top == now ? 1.f : fast_exp2(top - now), w = p.x == now ? 1.f : fast_exp2(p.x - now);
+    top = now;
+    sum = __fmaf_rn(p.y, w, sum * f);
+    acc.x = __fmaf_rn(y.x, w, acc.x * f);
+    acc.y = __fmaf_rn(y.y, w, acc.y * f);
+    acc.z = __fmaf_rn(y.z, w, acc.z * f);
+    acc.w = __fmaf_rn(y.w, w, acc.w * f);
   }
-  part[way][d] = acc.x;
-  part[way][d + 1] = acc.y;
-  part[way][d + 2] = acc.z;
-  part[way][d + 3] = acc.w;
-  if (d == 0) part[way][D] = sum;
+  *reinterpret_cast<float4*>(&part[way][d]) = acc;
+  if (d == 0) { part[way][D] = top; part[way][D + 1] = sum; }
   __syncthreads();
   if (way) return;
 #pragma unroll
-  for (uint32_t w = 1; w < kWays; ++w) {
-    acc.x += part[w][d];
-    acc.y += part[w][d + 1];
-    acc.z += part[w][d + 2];
-    acc.w += part[w][d + 3];
-  }
+  for (uint32_t w = 0; w < kWays; ++w) top = fmaxf(top, part[w][D]);
   sum = 0.f;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (uint32_t w = 0; w < kWays; ++w) sum += part[w][D];
+  for (uint32_t w = 0; w < kWays; ++w) {
+    const float f = part[w][D] == top ? 1.f : fast_exp2(part[w][D] - top);
+    const float4 y = *reinterpret_cast<const float4*>(&part[w][d]);
+    sum = __fmaf_rn(part[w][D + 1], f, sum);
+    acc.x = __fmaf_rn(y.x, f, acc.x);
+    acc.y = __fmaf_rn(y.y, f, acc.y);
+    acc.z = __fmaf_rn(y.z, f, acc.z);
+    acc.w = __fmaf_rn(y.w, f, acc.w);
+  }
   const float inv = 1.f / sum;
   *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
   if (lse && d == 0) *lse = (top - kOffset + log2f(sum)) * 0.693147180559945309f;

@@ -796,54 +796,53 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   if (warp == 9) tmem_free(tmem, 512);
 }
 
-// Joins the parts of the units that several blocks hold: a block of this kernel takes 32 rows of the unit whose
-// first part block x of the first kernel has, a warp four of them one after the other.
+// Joins the parts of the units that several blocks hold: a block of this kernel takes eight rows, a warp each, of the unit
+// whose first part block x of the first kernel has.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) prefill_join_kernel(const __grid_constant__ AttnArgs a, const Plan p) {
   constexpr int kPer = D / 32;
   const uint32_t lane = threadIdx.x % 32, c0 = blockIdx.x;
   wait_primary();
+  const Work w = p.split[c0].w;           // (read beside `parts`, whatever that says)
   const uint32_t parts = p.split[c0].parts;
   if (parts == 0) return;
-  const Work w = p.split[c0].w;
-#pragma unroll 1
-  for (uint32_t r = blockIdx.y * 32 + threadIdx.x / 32; r < blockIdx.y * 32 + 32; r += 8) {
-    const uint32_t i = r / 128, tok = r % 128 / a.group, head = w.h * a.group + r % 128 % a.group;
-    const int t = w.q0 + (int)(i * p.tq + tok);
-    if (tok >= p.tq || t >= w.n) continue;
-    // the first block holds its last unit's part, the others their first one's
-    auto at = [&](uint32_t k) { return (size_t)(2 * (c0 + k) + (k == 0 ? 1 : 0)) * 256 + r; };
-    float top = -INFINITY, sum = 0.f, acc[kPer];
-    for (uint32_t k = lane; k < parts; k += 32) top = fmaxf(top, p.part_ml[2 * at(k)]);
+  const uint32_t r = blockIdx.y * 8 + threadIdx.x / 32;
+  const uint32_t i = r / 128, tok = r % 128 / a.group, head = w.h * a.group + r % 128 % a.group;
+  const int t = w.q0 + (int)(i * p.tq + tok);
+  if (tok >= p.tq || t >= w.n) return;
+  // the first block holds its last unit's part, the others their first one's
+  auto at = [&](uint32_t k) { return (size_t)(2 * (c0 + k) + (k == 0 ? 1 : 0)) * 256 + r; };
+  float top = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll
-    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-#pragma unroll
-    for (int y = 0; y < kPer; ++y) acc[y] = 0.f;
+  for (int y = 0; y < kPer; ++y) acc[y] = 0.f;
 #pragma unroll 4
-    for (uint32_t k = 0; k < parts; ++k) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at(k));
-      if (ml.y == 0.f) continue;          // (it has no O)
-      const float f = ml.x == top ? 1.f : fast_exp2(ml.x - top);
-      sum = __fmaf_rn(ml.y, f, sum);
-      const float* o = p.part_o + at(k) * D + lane * kPer;
+  for (uint32_t k = 0; k < parts; ++k) {
+    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at(k));
+    float o[kPer];
 #pragma unroll
-      for (int y = 0; y < kPer; ++y) acc[y] = __fmaf_rn(o[y], f, acc[y]);
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    bool odd = false;
-    const size_t row = (size_t)(w.first + t);
-    T* out = static_cast<T*>(a.out) + row * a.out_stride + (size_t)head * D + lane * kPer;
+    for (int y = 0; y < kPer; ++y) o[y] = p.part_o[at(k) * D + lane * kPer + y];
+    if (ml.y == 0.f) continue;            // (it has no O: what was read is nothing)
+    const float now = fmaxf(top, ml.x);
+    const float f = top == now ? 1.f : fast_exp2(top - now), g = ml.x == now ? 1.f : fast_exp2(ml.x - now);
+    top = now;
+    sum = __fmaf_rn(ml.y, g, sum * f);
 #pragma unroll
-    for (int y = 0; y < kPer; y += 2) {
-      const float f = acc[y] * inv, g = acc[y + 1] * inv;
-      odd |= !(fabsf(f) < INFINITY) || !(fabsf(g) < INFINITY);
-      *reinterpret_cast<uint32_t*>(out + y) = pack2(f, g, T());
-    }
-    if (a.lse && lane == 0) a.lse[row * a.n_heads + head] = sum == 0.f ? -INFINITY : (top - kShift<T> + log2f(sum)) * 0.693147180559945309f;
-    // (a sum that is NaN: a wrong page, or a score that is none)
-    if (__any_sync(0xffffffffu, odd) && sum == sum)
-      mend_row<T, D>(a, w.s, w.kv - w.n + t, w.tiles[i] * kKeys, w.kv, (uint32_t)row, head, lane);
+    for (int y = 0; y < kPer; ++y) acc[y] = __fmaf_rn(o[y], g, acc[y] * f);
   }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  bool odd = false;
+  const size_t row = (size_t)(w.first + t);
+  T* out = static_cast<T*>(a.out) + row * a.out_stride + (size_t)head * D + lane * kPer;
+#pragma unroll
+  for (int y = 0; y < kPer; y += 2) {
+    const float f = acc[y] * inv, g = acc[y + 1] * inv;
+    odd |= !(fabsf(f) < INFINITY) || !(fabsf(g) < INFINITY);
+    *reinterpret_cast<uint32_t*>(out + y) = pack2(f, g, T());
+  }
+  if (a.lse && lane == 0) a.lse[row * a.n_heads + head] = sum == 0.f ? -INFINITY : (top - kShift<T> + log2f(sum)) * 0.693147180559945309f;
+  // (a sum that is NaN: a wrong page, or a score that is none)
+  if (__any_sync(0xffffffffu, odd) && sum == sum)
+    mend_row<T, D>(a, w.s, w.kv - w.n + t, w.tiles[i] * kKeys, w.kv, (uint32_t)row, head, lane);
 }
 
 // e4m3 pages as 16-bit rows [kv head][linear][D], a sequence after the other from multiples of 128 rows.
@@ -953,7 +952,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   prefill_kernel<T, D><<<sms, kThreads, Z::kBytes, st>>>(a, p, qm, km, vm);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(sms, 8);
+  cfg.gridDim = dim3(sms, 32);
   cfg.blockDim = dim3(256);
   cfg.stream = st;
   cudaLaunchAttribute early = {};
