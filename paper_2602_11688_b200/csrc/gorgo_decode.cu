@@ -9,7 +9,7 @@
 // blocks fit the GPU at once: no length and no batch leaves an SM idle, and at most two pieces of a block are
 // partial; a second, small kernel joins those (it starts early and waits for the first one's end).
 //
-// Each of a block's four warps takes a slice of every tile, 4 KB of keys as far as that is 32 at most, and is on
+// Each of a block's four warps takes a slice of every tile, 4 KB of keys (16 to 64), and is on
 // its own: its own ring of bulk copies, its own running maximum and sum; warps meet only at the end of a
 // (sequence, head).  Keys are the rows of the
 // matrix instructions (S^T = K q^T, O^T = V^T P^T, 16 x 8 x 16), so that up to eight query heads cost what one
@@ -28,14 +28,17 @@ constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr float kOffset = 14.f;           // p = 2^(z - m + kOffset): fp16 keeps p down to 2^-38 of the largest
 
-template <bool kQuant, int D>
+template <bool kQuant, int D, int NB>
 struct Sizes {
   static constexpr int kRow = D * (kQuant ? 1 : 2);            // bytes of a row
-  static constexpr int kSlice = kRow == 256 ? 16 : 32;         // keys of a warp in a tile
+  static constexpr int kSlice = 4096 / kRow;                   // keys of a warp in a tile
   static constexpr int kBlocks = kSlice / 16;
   static constexpr int kTile = kWarps * kSlice;
   static constexpr int kPart = kSlice * kRow;                  // K or V of a slice
-  static constexpr int kStages = kPart == 4096 ? 3 : 6;
+  // Codes take more instructions a byte, in chains that a scheduler with two warps does not fill: three blocks an SM
+  // with two stages each, where their registers allow it.
+  static constexpr int kPerSm = kQuant && NB == 1 ? 3 : 2;
+  static constexpr int kStages = kPerSm == 3 ? 2 : 3;
   static constexpr int kRing = kWarps * kStages * 2 * kPart;
   static constexpr int kPad = 64 + 4;                          // floats of a head's row in the merge buffer: 64 dims at a time
   static constexpr int kMerge = kWarps * 8 * kPad * 4;
@@ -115,9 +118,9 @@ __device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) {
 }
 
 template <typename T, bool kQuant, int D, int NB>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, Sizes<kQuant, D, NB>::kPerSm)
 decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-  using Z = Sizes<kQuant, D>;
+  using Z = Sizes<kQuant, D, NB>;
   using M = typename std::conditional<kQuant, __half, T>::type;   // type of the matrix instructions' operands
   constexpr int kSteps = D / 16, kH = 8 * NB, kSlice = Z::kSlice, kBlocks = Z::kBlocks;
   constexpr bool kLow = !(kQuant && std::is_same<T, __nv_bfloat16>::value);   // fp16 P is exact enough for a bf16 result
@@ -338,7 +341,8 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float x = fmaxf(c[0][nb][i], c[0][nb][i + 2]);
-          if (kBlocks == 2) x = fmaxf(x, fmaxf(c[kBlocks - 1][nb][i], c[kBlocks - 1][nb][i + 2]));
+#pragma unroll
+          for (int b = 1; b < kBlocks; ++b) x = fmaxf(x, fmaxf(c[b][nb][i], c[b][nb][i + 2]));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
@@ -589,12 +593,12 @@ uint32_t head_blocks(uint32_t group) { return group <= 8 ? 1 : (group + 15) / 16
 
 template <typename T, bool kQuant, int D, int NB>
 cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
-  using Z = Sizes<kQuant, D>;
-  static_assert(2 * (Z::kBytes + 1024) <= 233472, "two blocks an SM");
+  using Z = Sizes<kQuant, D, NB>;
+  static_assert(Z::kPerSm * (Z::kBytes + 1024) <= 233472, "blocks of an SM");
   Split sp;
   sp.ng = head_blocks(a.group);
   sp.hh = a.kv.n_kv_heads * sp.ng;
-  sp.grid = 2 * sms;
+  sp.grid = Z::kPerSm * sms;
   sp.box = min((uint32_t)Z::kSlice, 1u << a.kv.page_shift);
   sp.part_o = static_cast<float*>(a.workspace);
   sp.part_ml = sp.part_o + (size_t)2 * sp.grid * 8 * NB * D;
@@ -634,7 +638,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
 
 uint64_t decode_workspace(const AttnArgs& a, int sms) {
   const uint64_t heads = a.group <= 8 ? 8 : 16;
-  return (uint64_t)2 * 2 * sms * heads * (a.head_dim + 2) * 4;
+  return (uint64_t)2 * 3 * sms * heads * (a.head_dim + 2) * 4;   // (three blocks an SM at most, two parts each)
 }
 
 cudaError_t launch_attn_decode(const AttnArgs& a, int sms, cudaStream_t st) {
