@@ -496,7 +496,8 @@ const char *gorgo_strerror(int code);
  * between them.  All arrays are DEVICE memory of `device`.  The lengths and the table are read on the device: the
  * kernels check them, never leave the given arrays, and report what is wrong in `status` (bits
  * GORGO_KV_*, set and never cleared); outputs of a sequence with a wrong page or length hold NaN (attention, read) or its
- * wrong tokens are left out (write).  A page that is written must not be in the table twice in one batch. */
+ * wrong tokens are left out (write); rows of a sequence whose place in the packed array makes no sense are left as they
+ * are.  A page that is written must not be in the table twice in one batch. */
 enum { GORGO_BF16 = 0, GORGO_FP16 = 1, GORGO_E4M3 = 2 };
 enum {
   GORGO_KV_BAD_PAGE = 1,              /* a table entry that is needed is outside [0, n_pages)       */
@@ -552,7 +553,9 @@ int gorgo_kv_read(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch, 
  * unless that is e4m3), n_heads a multiple of n_kv_heads (at most 128 times as many), query head h reads kv head
  * h / (n_heads / n_kv_heads); row strides in elements, multiples of 8, 16-byte aligned.  With z_j = scale * (q . k_j)
  * over the keys j that a row sees: out = sum_j exp(z_j) v_j / sum_j exp(z_j), lse (DEVICE
- * float [rows][n_heads], or NULL) = log sum_j exp(z_j).  A row that sees no key gets zeros and -inf.
+ * float [rows][n_heads], or NULL) = log sum_j exp(z_j).  A row that sees no key gets zeros and -inf.  What a row does not
+ * see does not reach it, whatever it holds; a value it sees that is not finite makes that element of its result not finite
+ * (NaN or infinite), a score that is NaN or +inf the whole row.  GORGO_ERR_NONFINITE_PARAM: `scale` is not finite in 32 bits.
  *   gorgo_attn_prefill: one row per new token; the token at position p of its sequence sees the keys 0..p
  * (those of the new tokens are written first).  Rows behind cu_new[n_seqs] are left as they are.
  *   gorgo_attn_decode: one row per sequence, which sees all its kv_len[s] keys; cu_new, total_new and

@@ -85,7 +85,7 @@ bool batch_ok(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, bool decode)
   if (!b || b->reserved || b->n_seqs > 65535) return false;
   if (b->n_seqs == 0) return true;
   if (b->total_kv >= 1ull << 40) return false;
-  if (!b->kv_len || !b->table || (!decode && !b->cu_new)) return false;
+  if (!b->kv_len || (!b->table && b->max_kv) || (!decode && !b->cu_new)) return false;
   if (!decode && (b->total_new >= (1u << 24) || b->max_new > b->total_new)) return false;
   return b->max_kv < (1u << 24) && (uint64_t)b->table_stride * c->page_tokens >= b->max_kv;
 }
@@ -148,16 +148,17 @@ AttnArgs attn_args(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, uint32_
 int attend(bool decode, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, const void* q, uint32_t n_heads, uint32_t type,
            uint64_t qs, double scale, void* out, uint64_t os, float* lse, void* ws, uint64_t ws_bytes, void* stream) {
   if (!cache_ok(c) || !batch_ok(c, b, decode) || !type_ok(c, type) || !heads_ok(c, n_heads)) return GORGO_ERR_INVALID_ARG;
-  if (!std::isfinite(scale)) return GORGO_ERR_NONFINITE_PARAM;
+  const float scale_log2 = (float)(scale * 1.4426950408889634074);
+  if (!std::isfinite(scale_log2)) return GORGO_ERR_NONFINITE_PARAM;
   const uint64_t rows = b->n_seqs == 0 ? 0 : decode ? b->n_seqs : b->total_new;
   if (rows == 0) return GORGO_OK;
   const uint64_t width = (uint64_t)n_heads * c->head_dim;
   if (rows * n_heads >= (1ull << 31) || !rows_ok(q, qs, width) || !rows_ok(out, os, width)) return GORGO_ERR_INVALID_ARG;
+  AttnArgs a = attn_args(c, b, n_heads, type);
+  if (!decode && !prefill_fits(a)) return GORGO_ERR_INVALID_ARG;
   DeviceScope dev(c->device);
   const int sms = dev.ok ? sm_count(c->device) : 0;
   if (!sms) return GORGO_ERR_CUDA;
-  AttnArgs a = attn_args(c, b, n_heads, type);
-  if (!decode && !prefill_fits(a)) return GORGO_ERR_INVALID_ARG;
   const uint64_t need = (decode ? decode_workspace(a, sms) : prefill_workspace(a, sms));
   if (need && (!ws || !aligned(ws, 256))) return GORGO_ERR_INVALID_ARG;
   if (ws_bytes < need) return GORGO_ERR_WORKSPACE_TOO_SMALL;
@@ -166,7 +167,7 @@ int attend(bool decode, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, co
   a.lse = lse;
   a.q_stride = qs;
   a.out_stride = os;
-  a.scale_log2 = (float)(scale * 1.4426950408889634074);
+  a.scale_log2 = scale_log2;
   a.workspace = ws;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   return (decode ? launch_attn_decode(a, sms, st) : launch_attn_prefill(a, sms, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
@@ -193,10 +194,10 @@ int gorgo_attn_workspace_bytes(const gorgo_kv_cache_t* cache, const gorgo_kv_bat
     return GORGO_ERR_INVALID_ARG;
   *bytes_out = 0;
   if (batch->n_seqs == 0) return GORGO_OK;
-  const int sms = sm_count(cache->device);
-  if (!sms) return GORGO_ERR_CUDA;
   const AttnArgs a = attn_args(cache, batch, n_heads, type);
   if (!decode && !prefill_fits(a)) return GORGO_ERR_INVALID_ARG;
+  const int sms = sm_count(cache->device);
+  if (!sms) return GORGO_ERR_CUDA;
   *bytes_out = decode ? decode_workspace(a, sms) : prefill_workspace(a, sms);
   return GORGO_OK;
 }

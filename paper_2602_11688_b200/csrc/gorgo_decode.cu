@@ -210,6 +210,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
       }
     }
     get.next(a.b, sp.hh);
+    __syncwarp();                         // (bad_page is read by all lanes)
   };
 
   uint32_t flying = 0;                    // stages whose copies may still run

@@ -161,7 +161,9 @@ __device__ __forceinline__ uint32_t mma_shape(uint32_t n, bool bf16, bool negate
 // New rows of sequence s if its place in the packed array makes sense, else none.
 __device__ __forceinline__ int rows_of(const BatchView& b, uint32_t s) {
   const int a = b.cu_new[s], e = b.cu_new[s + 1];
-  return a < 0 || e < a || (uint32_t)e > b.total_new ? 0 : e - a;
+  if (a >= 0 && e >= a && (uint32_t)e <= b.total_new) return e - a;
+  report(b.status, GORGO_KV_BAD_LENGTH);
+  return 0;
 }
 
 // sum of floor((a i + b) / m) over 0 <= i < n, for 0 <= a, b: by the steps of Euclid's algorithm on (a, m).

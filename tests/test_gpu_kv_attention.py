@@ -115,6 +115,88 @@ def test_wrong_pages_and_lengths_are_reported(decode):
         check(out[keep], None, [w[keep] for w in want], BF16)
 
 
+@pytest.mark.parametrize("decode", [False, True])
+def test_a_row_that_is_in_no_place_is_reported_and_left(decode):
+    from paper_2602_11688_b200 import binding as gb
+    m = Made(71, [3, 4, 2], [30, 70, 40], page=16)
+    m.batch.cu_new[1:3] = torch.tensor([5, 4], dtype=torch.int32, device="cuda")      # decreasing: the second has no rows
+    if decode:                                               # which does not use them
+        check(m.cache.decode(m.batch, m.q[:3]), None, m.expected(m.q[:3], 0.125, True), BF16)
+        m.batch.check()
+        return
+    m.cache.prefill(m.batch, m.q)
+    assert int(m.batch.status.item()) == gb.GORGO_KV_BAD_LENGTH
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(128, 1, 64), (130, 2, 128), (99, 3, 64)])
+@pytest.mark.parametrize("store", [BF16, E4M3])
+def test_large_groups(heads, kv_heads, dim, store):
+    m = Made(73, [1, 5, 2], [140, 5, 300], heads=heads, kv_heads=kv_heads, dim=dim, store=store, page=32)
+    lse = torch.empty((8, heads), device="cuda")
+    check(m.cache.prefill(m.batch, m.q, lse=lse), lse, m.expected(m.q, dim ** -0.5, False), BF16)
+    lse = torch.empty((3, heads), device="cuda")
+    check(m.cache.decode(m.batch, m.q[:3], lse=lse), lse, m.expected(m.q[:3], dim ** -0.5, True), BF16)
+
+
+@pytest.mark.parametrize("dtype,store", [(BF16, BF16), (FP16, FP16), (BF16, E4M3), (FP16, E4M3)])
+def test_decode_with_what_is_not_finite(dtype, store):
+    """In a value: that element of the heads that read it; in a key or a query: those rows.  Nothing else."""
+    for what in ("value", "key", "query"):
+        m = Made(79, [1, 1, 1], [200, 700, 64], heads=6, kv_heads=2, dim=64, dtype=dtype, store=store, page=64)
+        want = m.expected(m.q, 0.125, True)
+        hit = torch.zeros((3, 6, 64), dtype=torch.bool, device="cuda")
+        pg, slot = m.where(1, torch.tensor([333], device="cuda"))
+        if what == "query":
+            m.q[1, 4, 7] = float("inf")
+            hit[1, 4] = True
+        else:
+            pool = m.cache.v if what == "value" else m.cache.k
+            if store == E4M3:
+                pool.view(torch.uint8)[pg, 0, slot, 11] = 0x7f
+            else:
+                pool[pg, 0, slot, 11] = float("nan")
+            hit[1, :3, slice(11, 12) if what == "value" else slice(None)] = True
+        out = m.cache.decode(m.batch, m.q)
+        assert not bool(torch.isfinite(out[hit]).any())
+        out[hit] = want[0][hit].to(dtype)
+        check(out, None, want, dtype)
+
+
+def test_sequences_without_tokens():
+    from paper_2602_11688_b200 import binding as gb
+    m = Made(83, [2], [2], heads=4, kv_heads=2, dim=64)
+    none = torch.zeros((2, 0), dtype=torch.int32, device="cuda")
+    batch = gb.GorgoKvBatch([0, 0], [0, 0], none)
+    assert m.cache.prefill(batch, m.q[:0]).shape == (0, 4, 64)
+    lse = torch.empty((2, 4), device="cuda")
+    out = m.cache.decode(batch, m.q, lse=lse)
+    assert bool((out == 0).all()) and bool((lse == -torch.inf).all())
+    batch = gb.GorgoKvBatch([2, 0], [0, 0], none)            # new rows of a sequence without tokens
+    lse = torch.empty((2, 4), device="cuda")
+    out = m.cache.prefill(batch, m.q, lse=lse)
+    assert bool((out == 0).all()) and bool((lse == -torch.inf).all())
+    batch.check()
+    assert [x.shape[0] for x in m.cache.read(gb.GorgoKvBatch([], [], none[:0]))] == [0, 0]
+
+
+def test_calls_side_by_side_on_several_streams():
+    """Calls that run at the same time have workspaces of their own."""
+    made = [Made(89 + i, [1, 40 + i, 7], [900 + i, 300, 7 + i], heads=8, kv_heads=2, dim=128, page=64,
+                 store=E4M3 if i % 2 else BF16) for i in range(4)]
+    first = [(m.cache.prefill(m.batch, m.q), m.cache.decode(m.batch, m.q[:3])) for m in made]
+    streams = [torch.cuda.Stream() for _ in made]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    again = [[] for _ in made]
+    for _ in range(20):
+        for m, s, a in zip(made, streams, again):
+            with torch.cuda.stream(s):
+                a.append((m.cache.prefill(m.batch, m.q), m.cache.decode(m.batch, m.q[:3])))
+    torch.cuda.synchronize()
+    for f, a in zip(first, again):
+        assert all(torch.equal(x, y) for pair in a for x, y in zip(pair, f))
+
+
 def test_the_same_call_gives_the_same_bits_and_streams_and_graphs_do_too():
     m = Made(59, [1] * 5, [3000, 17, 0, 900, 4097], heads=8, kv_heads=2, dim=128, page=128)
     n = Made(61, [300, 20], [2000, 20], heads=8, kv_heads=2, dim=128, page=128)

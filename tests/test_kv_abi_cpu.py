@@ -53,8 +53,13 @@ def test_bad_caches_are_refused(bad):
     assert rc == gb.GORGO_ERR_INVALID_ARG
 
 
+def test_sequences_without_tokens_need_no_table():
+    got = calls(cache(), batch(total_new=0, max_new=0, max_kv=0, total_kv=0, table=None, table_stride=0), p=None)
+    assert got["write"] == got["read"] == got["prefill"] == gb.GORGO_OK
+
+
 @pytest.mark.parametrize("bad", [
-    dict(reserved=1), dict(n_seqs=65536), dict(kv_len=None), dict(table=None), dict(table_stride=2), dict(max_kv=1 << 24)])
+    dict(reserved=1), dict(n_seqs=65536), dict(total_kv=1 << 40), dict(kv_len=None), dict(table=None), dict(table_stride=2), dict(max_kv=1 << 24)])
 def test_bad_batches_are_refused(bad):
     assert set(calls(cache(), batch(**bad)).values()) == {gb.GORGO_ERR_INVALID_ARG}
 
@@ -81,11 +86,19 @@ def test_heads_are_a_multiple_of_the_kv_heads(heads):
 
 @pytest.mark.parametrize("kw,code", [(dict(scale=float("nan")), gb.GORGO_ERR_NONFINITE_PARAM),
                                      (dict(scale=float("inf")), gb.GORGO_ERR_NONFINITE_PARAM),
+                                     (dict(scale=1e39), gb.GORGO_ERR_NONFINITE_PARAM),
                                      (dict(out_stride=255), gb.GORGO_ERR_INVALID_ARG),
                                      (dict(out_stride=248), gb.GORGO_ERR_INVALID_ARG)])
 def test_attention_refuses_bad_scales_and_outputs(kw, code):
     got = calls(cache(), batch(), **kw)
     assert got["prefill"] == got["decode"] == code
+
+
+def test_prefill_refuses_a_16_bit_copy_of_too_many_rows():
+    c = cache(type=gb.GORGO_E4M3, k_exp=A, v_exp=A, n_pages=1 << 20)
+    b = batch(total_kv=1 << 30)
+    assert calls(c, b)["prefill"] == gb.GORGO_ERR_INVALID_ARG
+    assert gb.gorgo_attn_workspace_bytes(c, b, 4, gb.GORGO_BF16, 0)[0] == gb.GORGO_ERR_INVALID_ARG
 
 
 def test_null_structures_are_refused():
