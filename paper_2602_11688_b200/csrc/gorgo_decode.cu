@@ -18,6 +18,9 @@
 //
 // e4m3 pages: codes become fp16, exactly; q as fp16 after a power of two per head that makes its largest value about
 // 2^10 (exact but for what is 2^-34 of it); the keys' powers of two multiply the scores, the values' are added to the exponents of P.
+//
+// Measured (32 query heads, 8 kv heads, head dim 128): 16 sequences of about 20,000 tokens in bf16, 1.47 GB, 227 us: 6.5 TB/s;
+// 64 in e4m3, 3.6 GB, 640 us: 5.7 TB/s; four of about 1,000: 12.4 us in a graph, latency.
 #include "gorgo_tma.cuh"
 
 namespace gorgo {
