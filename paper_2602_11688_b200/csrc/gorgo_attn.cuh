@@ -4,7 +4,6 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -94,10 +93,23 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, __half) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// Two e4m3 codes (low byte first) as floats, exactly.
-__device__ __forceinline__ float2 unpack_e4m3(uint32_t two) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-  return __half22float2(__half2(h));
+// Two e4m3 codes (low byte first) as fp16 and as floats, exactly.
+__device__ __forceinline__ uint32_t codes_to_half2(uint16_t two) {
+  uint32_t y;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(two));
+  return y;
+}
+__device__ __forceinline__ float2 unpack_e4m3(uint32_t two) { return unpack2(codes_to_half2((uint16_t)two), __half()); }
+
+// Four floats as e4m3 codes (the first in the low byte), each rounded to nearest even.
+__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {
+  uint32_t y;
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+      "mov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(y) : "f"(a), "f"(b), "f"(c), "f"(d));
+  return y;
 }
 
 // New tokens and all tokens of sequence s; a wrong length is reported and counts as no tokens.

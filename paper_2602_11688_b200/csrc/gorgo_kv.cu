@@ -116,9 +116,7 @@ __global__ void __launch_bounds__(kMoveThreads) kv_write_kernel(const KvMoveArgs
         uint32_t c[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i] * inv, f[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-          const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i + 2] * inv, f[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-          c[i] = lo | hi << 16;
+          c[i] = codes_of(f[4 * i] * inv, f[4 * i + 1] * inv, f[4 * i + 2] * inv, f[4 * i + 3] * inv);
         }
         if (top >= 0x7f800000u) c[0] = c[1] = 0x7f7f7f7fu;     // an infinity or NaN: the row is NaN
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + row * D + l * 8) = make_uint2(c[0], c[1]);
