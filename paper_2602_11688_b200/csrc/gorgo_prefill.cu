@@ -170,18 +170,18 @@ __device__ __forceinline__ int rows_of(const BatchView& b, uint32_t s) {
   return 0;
 }
 
-// sum of floor((a i + b) / m) over 0 <= i < n, for 0 <= a, b: by the steps of Euclid's algorithm on (a, m).
-__device__ uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+// sum of floor((a i + b) / m) over 0 <= i < n, for a n + b < 2^32: by the steps of Euclid's algorithm on (a, m).
+__device__ uint64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
   uint64_t sum = 0;
   while (n) {
-    sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+    sum += (uint64_t)n * (n - 1) / 2 * (a / m) + (uint64_t)n * (b / m);
     a %= m;
     b %= m;
-    const uint64_t y = a * n + b;
+    const uint32_t y = a * n + b;
     if (y < m) break;
     n = y / m;
     b = y % m;
-    const uint64_t t = m;
+    const uint32_t t = m;
     m = a;
     a = t;
   }
@@ -203,7 +203,7 @@ __device__ uint64_t places_before(int q, int step, int n, int kv) {
   }
   // units i < q: ceil((kv - n + (i + 1) step) / 128), none below zero
   const int none = kv < n ? (n - kv) / step : 0;               // units whose last token sees nothing
-  if (q > none) sum += floor_sum(q - none, kKeys, step, (uint64_t)(kv - n + (none + 1) * step + kKeys - 1));
+  if (q > none) sum += floor_sum(q - none, kKeys, step, (uint32_t)(kv - n + (none + 1) * step + kKeys - 1));
   return sum;
 }
 

@@ -162,6 +162,30 @@ def test_decode_with_what_is_not_finite(dtype, store):
         check(out, None, want, dtype)
 
 
+@pytest.mark.parametrize("store", [BF16, E4M3])
+def test_many_short_sequences(store):
+    """More sequences than a warp looks at at once, some without new tokens, some without any."""
+    import numpy as np
+    rng = np.random.default_rng(97)
+    new = [int(x) for x in rng.integers(0, 4, 333)]
+    kv = [n + int(x) if x else n for n, x in zip(new, rng.integers(0, 40, 333))]
+    kv[7] = new[7] = kv[200] = new[200] = 0
+    m = Made(97, new, kv, heads=4, kv_heads=2, dim=64, page=16, store=store)
+    check(m.cache.prefill(m.batch, m.q), None, m.expected(m.q, 0.125, False), BF16)
+    q = m.q[:333]
+    check(m.cache.decode(m.batch, q), None, m.expected(q, 0.125, True), BF16)
+    m.batch.check()
+
+
+def test_lengths_that_cut_the_line_everywhere():
+    """Prompts whose units and parts begin at every kind of place: short last units, tiles before the first one seen."""
+    for seed, heads, kv_heads in ((101, 7, 1), (103, 4, 4), (107, 24, 1)):
+        new = [1000, 3, 517, 129, 64, 1]
+        kv = [1000, 4000, 516, 2000, 63, 9000]
+        m = Made(seed, new, kv, heads=heads, kv_heads=kv_heads, dim=128, page=128)
+        check(m.cache.prefill(m.batch, m.q), None, m.expected(m.q, 128 ** -0.5, False), BF16)
+
+
 def test_sequences_without_tokens():
     from paper_2602_11688_b200 import binding as gb
     m = Made(83, [2], [2], heads=4, kv_heads=2, dim=64)
