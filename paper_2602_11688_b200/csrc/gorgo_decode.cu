@@ -54,6 +54,7 @@ struct Split {
   uint32_t ng;                            // blocks of query heads of a kv head
   float* part_o;                          // [2 * grid][8 * NB][D]
   float* part_ml;                         // [2 * grid][8 * NB][2]
+  uint4* first;                           // [grid]: the (sequence, pair) whose first part a block has, blocks that hold parts (0: none)
   uint32_t grid;                          // blocks of the first kernel
   uint32_t box;                           // keys of one bulk copy: a slice, or a page where that is less
 };
@@ -139,18 +140,35 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
   }
   launch_dependents();
 
+  // sequences without keys: zeros; with a wrong length: NaN
+  for (uint32_t s = blockIdx.x; s < a.b.n_seqs; s += gridDim.x) {
+    const int kv = a.b.kv_len[s];
+    const bool ok = kv_len_ok(a.b, kv);
+    if (ok && kv > 0) continue;
+    if (!ok && threadIdx.x == 0) report(a.b.status, GORGO_KV_BAD_LENGTH);
+    const uint32_t none = pack2(ok ? 0.f : NAN, ok ? 0.f : NAN, T());
+    uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + (size_t)s * a.out_stride);
+    for (uint32_t x = threadIdx.x; x < a.n_heads * (D / 2); x += kThreads) out[x] = none;
+    if (a.lse)
+      for (uint32_t x = threadIdx.x; x < a.n_heads; x += kThreads) a.lse[(size_t)s * a.n_heads + x] = ok ? -INFINITY : NAN;
+  }
+
   // this block's piece of the line, found by every warp for itself
   Iter<Z::kTile> use;
-  uint64_t seg_first;                     // first tile of sequence use.s on the line
+  uint64_t total = 0, at;                 // `at`: place of tile use.tile on the line
+  uint32_t n_pieces;
   {
-    uint64_t total = 0;
     for (uint32_t s = lane; s < a.b.n_seqs; s += 32) total += tiles_of<Z::kTile>(a.b, s);
 #pragma unroll
     for (int d = 16; d; d /= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
     total *= sp.hh;
-    const uint32_t n = pieces(total, gridDim.x);
-    if (blockIdx.x >= n || total == 0) return;
+    const uint32_t n = n_pieces = pieces(total, gridDim.x);
+    if (blockIdx.x >= n || total == 0) {
+      if (threadIdx.x == 0) sp.first[blockIdx.x] = make_uint4(0, 0, 0, 0);
+      return;
+    }
     const uint64_t lo = total * blockIdx.x / n, hi = total * (blockIdx.x + 1) / n;
+    at = lo;
     uint64_t before = 0;
     uint32_t s0 = 0, mine = 0, here = 0;
     for (;; s0 += 32) {                   // the sequence that holds tile `lo`
@@ -172,8 +190,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
     use.s = s0 + here;
     use.nt = __shfl_sync(0xffffffffu, mine, here);
     use.kv = a.b.kv_len[use.s];
-    seg_first = before * sp.hh;
-    const uint64_t off = lo - seg_first;
+    const uint64_t off = lo - before * sp.hh;
     use.hh = (uint32_t)(off / use.nt);
     use.tile = (uint32_t)(off % use.nt);
     use.left = (uint32_t)(hi - lo);
@@ -216,6 +233,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
   uint32_t qf[NB][kSteps][2];             // q as the second operand: (k = dim, n = head)
   float o[NB][kSteps][4], m[NB][2], l[NB][2], zs[NB][2];
   uint32_t st = 0, phase = 0, first_tile = 0, h0 = 0, n_h = 0;  // h0, n_h: first query head and how many
+  uint4 begun = make_uint4(0, 0, 0, 0);
   bool fresh = true, bad = false, alive = true;
   for (;;) {
     if (fresh) {
@@ -433,6 +451,10 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
       // the warps' sums of this (sequence, head) become one, eight heads and 64 dims at a time
       const bool whole = first_tile == 0 && use.tile + 1 == use.nt;
       const uint32_t slot = 2 * blockIdx.x + (first_tile == 0 ? 1 : 0);
+      if (!whole && first_tile == 0) {    // the second kernel finds its parts here and in the blocks behind
+        const uint64_t end = at + (use.nt - use.tile);         // of its tiles on the line
+        begun = make_uint4(use.s, use.hh, (uint32_t)((end * n_pieces - 1) / total) - blockIdx.x + 1, 0);
+      }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if (8 * nb >= (int)n_h) break;
@@ -495,58 +517,28 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
     }
     if (last) break;
     use.next(a.b, sp.hh);
+    ++at;
   }
+  if (threadIdx.x == 0) sp.first[blockIdx.x] = begun;
 }
 
-// Joins what several blocks hold of one query head, and answers for sequences without keys.  A block a head: its
-// threads take every 8th or 16th part, 16 bytes of the row each, with a running maximum, so that parts arrive side by side.
+// Joins what several blocks hold of one query head: block x of this kernel has the pair whose first part block x of the
+// first kernel has.  Its threads take every 8th or 16th part, 16 bytes of the row each, with a running maximum, so that
+// parts arrive side by side.
 constexpr int kJoinThreads = 256;
-template <typename T, int kTile, int D, int NB>
+template <typename T, int D, int NB>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArgs a, const Split sp) {
   constexpr uint32_t kH = 8 * NB, kVec = D / 4, kWays = kJoinThreads / kVec;
-  const uint32_t s = blockIdx.x / sp.hh, hh = blockIdx.x % sp.hh, h = blockIdx.y;
-  if (h >= a.group - hh % sp.ng * kH) { wait_primary(); return; }
-  const uint32_t head = hh / sp.ng * a.group + hh % sp.ng * kH + h;
-  const uint32_t way = threadIdx.x / kVec, d = threadIdx.x % kVec * 4;
-  constexpr uint32_t kJoinWarps = kJoinThreads / 32;
-  __shared__ unsigned long long sums[2][kJoinWarps];
+  const uint32_t way = threadIdx.x / kVec, d = threadIdx.x % kVec * 4, h = blockIdx.y;
   __shared__ float part[kWays][D + 4];
-  uint64_t before = 0, total = 0;
-  for (uint32_t x = threadIdx.x; x < a.b.n_seqs; x += kJoinThreads) {
-    const uint32_t n = tiles_of<kTile>(a.b, x);
-    total += n;
-    if (x < s) before += n;
-  }
-#pragma unroll
-  for (int i = 16; i; i /= 2) {
-    total += __shfl_xor_sync(0xffffffffu, total, i);
-    before += __shfl_xor_sync(0xffffffffu, before, i);
-  }
-  if (threadIdx.x % 32 == 0) { sums[0][threadIdx.x / 32] = before; sums[1][threadIdx.x / 32] = total; }
-  __syncthreads();
-  before = total = 0;
-#pragma unroll
-  for (uint32_t i = 0; i < kJoinWarps; ++i) {
-    before += sums[0][i];
-    total += sums[1][i];
-  }
-  total *= sp.hh;
-  const uint32_t nt = tiles_of<kTile>(a.b, s);
-  const uint32_t n = pieces(total, sp.grid);
+  wait_primary();
+  const uint4 what = sp.first[blockIdx.x];
+  const uint32_t s = what.x, hh = what.y;
+  if (what.z == 0 || h >= a.group - hh % sp.ng * kH) return;
+  const uint32_t head = hh / sp.ng * a.group + hh % sp.ng * kH + h;
+  const uint32_t c0 = blockIdx.x, c1 = c0 + what.z - 1;
   T* out = static_cast<T*>(a.out) + (size_t)s * a.out_stride + (size_t)head * D + d;
   float* lse = a.lse ? a.lse + (size_t)s * a.n_heads + head : nullptr;
-  wait_primary();
-  if (nt == 0) {
-    const bool ok = kv_len_ok(a.b, a.b.kv_len[s]);
-    if (!ok && threadIdx.x == 0) report(a.b.status, GORGO_KV_BAD_LENGTH);
-    const uint32_t none = pack2(ok ? 0.f : NAN, ok ? 0.f : NAN, T());
-    if (way == 0) *reinterpret_cast<uint2*>(out) = make_uint2(none, none);
-    if (lse && threadIdx.x == 0) *lse = ok ? -INFINITY : NAN;
-    return;
-  }
-  const uint64_t lo = before * sp.hh + (uint64_t)hh * nt, hi = lo + nt;   // its tiles on the line
-  const uint32_t c0 = (uint32_t)(((lo + 1) * n - 1) / total), c1 = (uint32_t)((hi * n - 1) / total);   // blocks that hold them
-  if (c0 == c1) return;
   // the first block holds its last piece of line, the others their first
   auto at = [&](uint32_t c) { return (size_t)(2 * c + (c == c0 ? 1 : 0)) * kH + h; };
   float top = -INFINITY, sum = 0.f;
@@ -600,6 +592,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   sp.box = min((uint32_t)Z::kSlice, 1u << a.kv.page_shift);
   sp.part_o = static_cast<float*>(a.workspace);
   sp.part_ml = sp.part_o + (size_t)2 * sp.grid * 8 * NB * D;
+  sp.first = reinterpret_cast<uint4*>(sp.part_ml + (size_t)2 * sp.grid * 8 * NB * 2);
   CUtensorMap km, vm;
   const uint64_t rows = (uint64_t)a.kv.n_pages * a.kv.n_kv_heads << a.kv.page_shift;
   const uint32_t planes = Z::kRow > 128 ? Z::kRow / 128 : 1;
@@ -612,7 +605,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   kernel<<<sp.grid, kThreads, Z::kBytes, st>>>(a, sp, km, vm);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.b.n_seqs * sp.hh, a.group < 8 * NB ? a.group : 8 * NB);
+  cfg.gridDim = dim3(sp.grid, a.group < 8 * NB ? a.group : 8 * NB);
   cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
   cudaLaunchAttribute early = {};
@@ -620,7 +613,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   early.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, Z::kTile, D, NB>, a, sp);
+  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, D, NB>, a, sp);
 }
 
 template <typename T, bool kQuant, int D>
@@ -636,7 +629,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
 
 uint64_t decode_workspace(const AttnArgs& a, int sms) {
   const uint64_t heads = a.group <= 8 ? 8 : 16;
-  return (uint64_t)2 * 3 * sms * heads * (a.head_dim + 2) * 4;   // (three blocks an SM at most, two parts each)
+  return (uint64_t)3 * sms * (2 * heads * (a.head_dim + 2) * 4 + 16);   // (three blocks an SM at most, two parts each)
 }
 
 cudaError_t launch_attn_decode(const AttnArgs& a, int sms, cudaStream_t st) {
