@@ -551,7 +551,8 @@ int gorgo_kv_read(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch, 
 
 /* Attention of queries against the pages.  q, out: DEVICE rows of `type` (bf16 or fp16; the cache's own
  * unless that is e4m3), n_heads a multiple of n_kv_heads (at most 128 times as many), query head h reads kv head
- * h / (n_heads / n_kv_heads); row strides in elements, multiples of 8, 16-byte aligned.  With z_j = scale * (q . k_j)
+ * h / (n_heads / n_kv_heads); row strides in elements, multiples of 8, 16-byte aligned; out does not overlap
+ * q.  With z_j = scale * (q . k_j)
  * over the keys j that a row sees: out = sum_j exp(z_j) v_j / sum_j exp(z_j), lse (DEVICE
  * float [rows][n_heads], or NULL) = log sum_j exp(z_j).  A row that sees no key gets zeros and -inf.  What a row does not
  * see does not reach it, whatever it holds; a value it sees that is not finite makes that element of its result not finite

@@ -537,7 +537,7 @@ class GorgoKvBatch:
         for x, m in ((cu_new, n + 1), (kv_len, n)):
             if x.dtype != torch.int32 or x.shape != (m,) or not x.is_contiguous() or x.device != dev:
                 raise ValueError("cu_new [sequences + 1] and kv_len [sequences]: int32, contiguous, beside the table")
-        self.n_seqs, self.total_new, self.device = n, sum(new), dev
+        self.n_seqs, self.total_new, self.device, self.columns = n, sum(new), dev, table.shape[1]
         self.table, self.cu_new, self.kv_len = table, cu_new, kv_len
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.c = gorgo_kv_batch_t(n, self.total_new, max(new, default=0), max(kv, default=0), sum(kv),
@@ -591,6 +591,11 @@ class GorgoKvCache:
             if dtype == torch.float8_e4m3fn else [None, None]
         return cls(*pools, *exps)
 
+    def _check(self, batch):
+        """The kernels check what the lengths and the table hold; here only that they are where they are looked for."""
+        if batch.device != self.device or batch.c.max_kv > batch.columns * self.page_tokens:
+            raise ValueError("batch: on the cache's GPU, with a table entry for every page of its longest sequence")
+
     def _rows(self, x, n, heads, what):
         """The C type of rows [n or more, heads, head dim] whose heads lie one after the other."""
         shape, strides, t = x.shape, x.stride(), self._types.get(x.dtype)
@@ -605,6 +610,7 @@ class GorgoKvCache:
 
     def write(self, batch, k_new, v_new):
         """Keys and values [new tokens, kv heads, head dim] of the batch's new tokens into their pages."""
+        self._check(batch)
         t = self._rows(k_new, batch.total_new, self.n_kv_heads, "k_new")
         if self._rows(v_new, batch.total_new, self.n_kv_heads, "v_new") != t:
             raise ValueError("k_new and v_new: one type")
@@ -616,6 +622,7 @@ class GorgoKvCache:
     def read(self, batch, dtype=None, out=None):
         """Keys and values of the batch's new tokens as (k, v), each [new tokens, kv heads, head dim]."""
         torch = self.torch
+        self._check(batch)
         if out is None:
             dtype = dtype or (self.dtype if self.dtype in self._types else torch.bfloat16)
             shape = (batch.total_new, self.n_kv_heads, self.head_dim)
@@ -640,6 +647,7 @@ class GorgoKvCache:
 
     def _attend(self, batch, q, scale, out, lse, rows, decode):
         torch, lib = self.torch, self._lib
+        self._check(batch)
         heads = q.shape[1] if q.dim() == 3 else 0
         t = self._rows(q, rows, heads, "q")
         if out is None:

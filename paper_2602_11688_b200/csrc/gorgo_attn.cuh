@@ -55,7 +55,6 @@ struct AttnArgs {
   uint32_t n_heads, group;                // group: query heads of a kv head
   uint32_t head_dim, type, store;
   float scale_log2;                       // scale * log2(e)
-  uint32_t max_new;
   uint64_t total_kv;
   void* workspace;
 };
@@ -73,10 +72,6 @@ __device__ __forceinline__ void report(uint32_t* status, uint32_t bits) {
 
 // 2^e for -126 <= e <= 127, exactly.
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }
-
-template <typename T> struct Half2Of;
-template <> struct Half2Of<__nv_bfloat16> { using type = __nv_bfloat162; };
-template <> struct Half2Of<__half> { using type = __half2; };
 
 __device__ __forceinline__ float2 unpack2(uint32_t x, __nv_bfloat16) {
   return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));

@@ -140,7 +140,6 @@ AttnArgs attn_args(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, uint32_
   a.head_dim = c->head_dim;
   a.type = type;
   a.store = c->type;
-  a.max_new = b->max_new;
   a.total_kv = b->total_kv;
   return a;
 }

@@ -96,6 +96,44 @@ def test_rows_with_a_nan_or_an_infinity_are_nan_in_e4m3():
         assert bool((o[~nan] == 1).all())
 
 
+def test_the_holders_refuse_what_does_not_fit():
+    from paper_2602_11688_b200 import binding as gb
+    cache, batch, table = make(9, [(3, 40), (2, 2)], 2, 64, BF16, 16)
+    x, q = (torch.zeros((5, h, 64), dtype=BF16, device="cuda") for h in (2, 4))
+    for bad in (x[:4], x[:, :1], x.to(FP16), x.float(), x.cpu(), torch.zeros((5, 2, 128), dtype=BF16, device="cuda"),
+                x.transpose(0, 1).contiguous().transpose(0, 1)):
+        with pytest.raises((ValueError, gb.GorgoError)):
+            cache.write(batch, bad, bad)
+        with pytest.raises((ValueError, gb.GorgoError)):
+            cache.read(batch, out=(bad, bad))
+    with pytest.raises(ValueError):
+        cache.write(batch, x, x.to(FP16))
+    for bad in (q[:4], q[:, :3], q.to(FP16), q[0], q.float()):
+        with pytest.raises((ValueError, gb.GorgoError)):
+            cache.prefill(batch, bad)
+    for kw in (dict(out=q[:4]), dict(out=q.to(FP16)), dict(lse=torch.zeros((5, 4), device="cuda").half()),
+               dict(lse=torch.zeros((4, 4), device="cuda")), dict(scale=float("nan"))):
+        with pytest.raises((ValueError, gb.GorgoError)):
+            cache.prefill(batch, q, **kw)
+    # a table that ends before the longest sequence does, although the rows behind it are long enough
+    wide = torch.zeros((2, 9), dtype=torch.int32, device="cuda")
+    short = gb.GorgoKvBatch([3, 2], [40, 2], wide[:, :2])
+    with pytest.raises(ValueError):
+        cache.prefill(short, q)
+    for args in (([1], [1, 2], table), ([-1, 1], [1, 2], table), ([1, 1], [1, 2], table.long()), ([1], [1], table),
+                 ([1, 1], [1, 2], table.cpu())):
+        with pytest.raises(ValueError):
+            gb.GorgoKvBatch(*args)
+    with pytest.raises(ValueError):
+        gb.GorgoKvBatch([1, 1], [1, 2], table, kv_len=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    for args in ((cache.k, cache.v[:1]), (cache.k, cache.v.to(FP16)), (cache.k.float(), cache.v.float()), (cache.k[:, :1], cache.v[:, :1]),
+                 (cache.k.to(E4M3), cache.v.to(E4M3)), (cache.k, cache.v, torch.zeros(3), None)):
+        with pytest.raises(ValueError):
+            gb.GorgoKvCache(*args)
+    with pytest.raises(gb.GorgoError):                       # pages of a size that the kernels do not have
+        gb.GorgoKvCache.empty(4, 2, 64, BF16, 48).write(gb.GorgoKvBatch([5], [5], table[:1]), x, x)
+
+
 def test_many_tokens_and_many_sequences():
     lengths = [(int(n), int(n) + int(m)) for n, m in zip(torch.randint(0, 9, (700,), generator=torch.Generator().manual_seed(1)),
                                                           torch.randint(0, 40, (700,), generator=torch.Generator().manual_seed(2)))]
