@@ -881,7 +881,7 @@ __global__ void __launch_bounds__(256) widen_kernel(const AttnArgs a, const uint
     if (lane == 0) { seq = s; tile = t; }
   }
   __syncthreads();
-  if (seq >= a.b.n_seqs) return;
+  if (seq >= a.b.n_seqs || rows_of(a.b, seq) == 0) return;     // (nobody reads it)
   const int kv = a.b.kv_len[seq];
   const uint32_t h = blockIdx.y, l = threadIdx.x % kLanes;
 #pragma unroll 4
@@ -889,10 +889,16 @@ __global__ void __launch_bounds__(256) widen_kernel(const AttnArgs a, const uint
     const uint32_t j = tile * kKeys + r;
     if ((int)j >= kv) break;
     const int64_t from = pool_row(a.kv, a.b, seq, h, j);
-    if (from < 0) continue;               // (reported by the attention kernel of that sequence)
     const size_t to = (size_t)h * linear + (size_t)blockIdx.x * kKeys + r;
+    if (from < 0) report(a.b.status, GORGO_KV_BAD_PAGE);       // the attention kernel does not look at the table: rows that
+                                                               // see this key are NaN because the key is
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
+      uint4* out = reinterpret_cast<uint4*>((v ? v_out : k_out) + to * D + l * 8);
+      if (from < 0) {
+        *out = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+        continue;
+      }
       const uint2 x = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(v ? a.kv.v : a.kv.k) + from * D + l * 8));
       const float f = pow2i((v ? a.kv.v_exp : a.kv.k_exp)[from]);
       uint32_t u[4];
@@ -901,7 +907,7 @@ __global__ void __launch_bounds__(256) widen_kernel(const AttnArgs a, const uint
         const float2 y = unpack_e4m3((i < 2 ? x.x : x.y) >> 16 * (i & 1) & 0xffffu);
         u[i] = pack2(y.x * f, y.y * f, T());
       }
-      *reinterpret_cast<uint4*>((v ? v_out : k_out) + to * D + l * 8) = make_uint4(u[0], u[1], u[2], u[3]);
+      *out = make_uint4(u[0], u[1], u[2], u[3]);
     }
   }
 }
