@@ -495,9 +495,9 @@ const char *gorgo_strerror(int code);
  * The calls only enqueue kernels on `cuda_stream` (they may be captured into a graph) and keep nothing
  * between them.  All arrays are DEVICE memory of `device`.  The lengths and the table are read on the device: the
  * kernels check them, never leave the given arrays, and report what is wrong in `status` (bits
- * GORGO_KV_*, set and never cleared); outputs of a sequence with a wrong page or length hold NaN (attention, read) or its
- * wrong tokens are left out (write); rows of a sequence whose place in the packed array makes no sense are left as they
- * are.  A page that is written must not be in the table twice in one batch. */
+ * GORGO_KV_*, set and never cleared); outputs that need a wrong page (attention: the rows that see a token of it) and all
+ * outputs of a sequence with a wrong length hold NaN (attention, read) or the wrong tokens are left out (write); rows of a
+ * sequence whose place in the packed array makes no sense are left as they are.  A page that is written must not be in the table twice in one batch. */
 enum { GORGO_BF16 = 0, GORGO_FP16 = 1, GORGO_E4M3 = 2 };
 enum {
   GORGO_KV_BAD_PAGE = 1,              /* a table entry that is needed is outside [0, n_pages)       */

@@ -73,10 +73,12 @@ struct Work {                             // a unit, or a block's part of it
   int tiles[2];                           // tiles of keys of either tile of rows, from 0
   int lo, hi;                             // the block's share of them
   uint32_t slot;                          // where a part goes; kWhole: the result is written
-  uint32_t bad, last;                     // a wrong page or length; nothing comes after the one before
+  int none_from;                          // first key that has no page: rows at this position or behind it are NaN
+  uint32_t last;                          // nothing comes after the one before
   uint64_t base;                          // first row of the sequence in the 16-bit copy
 };
 constexpr uint32_t kWhole = 0xffffffffu;
+constexpr int kAllKeys = 0x7fffffff, kNoRow = -kAllKeys - 1;   // none_from: every key has a page; a wrong length, all rows are NaN
 
 struct Split {                            // a unit whose first part a block has: what the second kernel needs
   Work w;
@@ -304,7 +306,7 @@ struct Walk {
       w.kv = seq.kv;
       w.q0 = q * step;
       w.base = base * kKeys;
-      w.bad = seq.bad || (p.linear && w.base + seq.kv > p.linear);
+      w.none_from = seq.bad || (p.linear && w.base + seq.kv > p.linear) ? kNoRow : kAllKeys;
       w.last = 0;
       for (int i = 0; i < 2; ++i) {
         const int t = w.q0 + i * (int)p.tq;                    // first token of the tile
@@ -539,7 +541,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         o_phase ^= 1;
         fence_after();
       }
-      const bool bad = w.bad != 0 || !go;
+      const bool bad = pos >= w.none_from || !go;
       if (w.slot != kWhole) {
         const size_t part = (size_t)w.slot * 256 + i * 128 + r;
         *reinterpret_cast<float2*>(p.part_ml + 2 * part) = make_float2(m * c, bad ? NAN : l);
@@ -611,14 +613,16 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         auto row_of = [&](int j) -> int64_t {
           const int key = (w.lo + j) * kKeys + (int)(lane * p.box);
           if (j >= most || lane >= most_pieces || key >= w.kv) return -2;
-          if (p.linear) return w.bad ? 0 : (int64_t)(w.h * p.linear + w.base + key);
+          if (p.linear) return w.none_from == kNoRow ? 0 : (int64_t)(w.h * p.linear + w.base + key);
           return pool_row(a.kv, a.b, w.s, w.h, (uint32_t)key);
         };
         int64_t row = row_of(0);
         for (int j = 0; go && j < most; ++j) {
+          const uint32_t wrong = __ballot_sync(0xffffffffu, row == -1);
           if (row == -1) {                // a wrong page: copies something that is there, and says so
             report(a.b.status, GORGO_KV_BAD_PAGE);
-            ring[e].bad = 1;
+            const int key = (w.lo + j) * kKeys + (int)(lane * p.box);
+            if (lane == (uint32_t)__ffs(wrong) - 1 && key < ring[e].none_from) ring[e].none_from = key;
             row = 0;
           }
           const uint32_t pieces = __popc(__ballot_sync(0xffffffffu, row >= 0));
@@ -764,7 +768,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         if (lane == 0) {
           if (more) {
             ring[e] = w;
-            if (w.bad) report(a.b.status, GORGO_KV_BAD_LENGTH);
+            if (w.none_from == kNoRow) report(a.b.status, GORGO_KV_BAD_LENGTH);
             if (w.slot != kWhole && w.lo == 0) {               // the second kernel finds its parts here and in the blocks behind
               parts = 1 + walk.blocks_after();
               p.split[blockIdx.x].w = w;

@@ -77,7 +77,7 @@ __device__ __forceinline__ void mend_row(const AttnArgs& a, uint32_t s, int pos,
   bool cause = false;
   for (int j = max(pos + 1, 0); j < min(end, kv); ++j) {
     const int64_t at = pool_row(a.kv, a.b, s, h / a.group, j);
-    if (at < 0) return;
+    if (at < 0) { cause = true; break; }  // (its stand-in may be anything)
     float v[kPer];
     load_row<T, D>(a.kv.v, a.kv.v_exp, at, lane, v);
 #pragma unroll

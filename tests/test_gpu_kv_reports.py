@@ -36,3 +36,19 @@ def test_a_wrong_page_or_length_in_every_type_of_cache(dtype, store, decode, fau
             assert bool(torch.isnan(o[3:7]).all())
             o, ref = (torch.cat([x[:3], x[7:]]) for x in (o, ref))
         assert torch.equal(o, ref)
+
+
+@pytest.mark.parametrize("store", [BF16, E4M3])
+def test_rows_that_see_a_wrong_page_and_rows_before_it(store):
+    from paper_2602_11688_b200 import binding as gb
+    for at in (0, 40, 130, 200, 299):
+        m = Made(57, [300, 40], [300, 200], heads=4, kv_heads=2, dim=64, page=16, store=store)
+        want = m.expected(m.q, 0.125, False)
+        m.batch.table[0, at // 16] = m.cache.n_pages
+        for _ in range(3):
+            out = m.cache.prefill(m.batch, m.q)
+            assert int(m.batch.status.item()) == gb.GORGO_KV_BAD_PAGE
+            first = at // 16 * 16
+            assert bool(torch.isnan(out[first:300]).all())
+            keep = list(range(first)) + list(range(300, 340))
+            check(out[keep], None, [w[keep] for w in want], BF16)
