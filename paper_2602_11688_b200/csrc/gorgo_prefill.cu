@@ -493,9 +493,13 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         float now = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
         const bool grow = !(now <= m + slack);                 // (also for NaN)
         if (__any_sync(0xffffffffu, grow)) {
-          if (now == INFINITY) now = NAN;                      // infinity - infinity: the row is NaN
-          const float f = grow ? fast_exp2((m - now) * c) : 1.f;
-          if (grow) m = now;
+          // m * c stays finite: a score beyond 32 bits makes the row NaN, below them it is minus infinity
+          const float z = now * c;
+          if (z == INFINITY) now = NAN;
+          if (z == -INFINITY) now = -INFINITY;
+          const bool up = grow && now != m;
+          const float f = up ? fast_exp2(m * c - now * c) : 1.f;
+          if (up) m = now;
           l *= f;
           if (j > 0) {
 #pragma unroll

@@ -1,0 +1,40 @@
+"""The paged key-value cache's attention at the ends of its numbers' ranges."""
+import pytest
+import torch
+
+from tests.kv_util import BF16, E4M3, FP16, Made, check, half_step, power, quantise
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [(BF16, BF16), (FP16, FP16), (BF16, E4M3), (FP16, E4M3)]
+
+
+def refill(m, pool, exps, kept, s, x):
+    """Sequence s's keys or values become the rows of x, as the cache holds them."""
+    at, slot = m.where(s, torch.arange(x.shape[0], device="cuda"))
+    if m.store == E4M3:
+        codes, e = quantise(x)
+        pool.view(torch.uint8)[at, :, slot] = codes.to(E4M3).view(torch.uint8)
+        exps[at, :, slot] = e.to(torch.int8)
+        kept[s] = codes * power(e[..., None])
+    else:
+        pool[at, :, slot] = x.to(m.store)
+        kept[s] = x.to(m.store).double()
+
+
+def attend(m, decode, q, scale):
+    n = len(m.kv) if decode else sum(m.new)
+    l = torch.zeros((n, m.heads), device="cuda")
+    out = (m.cache.decode if decode else m.cache.prefill)(m.batch, q, scale, lse=l)
+    m.batch.check()
+    return out, l
+
+
+@pytest.mark.parametrize("dtype,store", TYPES)
+@pytest.mark.parametrize("decode", [False, True])
+def test_scores_beyond_32_bits(dtype, store, decode):
+    m = Made(59, [1, 3, 140], [1, 200, 140], heads=4, kv_heads=2, dim=64, dtype=dtype, store=store, page=64)
+    for s, n in enumerate(m.kv):
+        refill(m, m.cache.k, m.cache.k_exp, m.keys, s, torch.ones((n, 2, 64), device="cuda"))
+    out, lse = attend(m, decode, torch.ones_like(m.q), 1e37)                # scores of 64 * 1e37
+    assert not bool(torch.isfinite(out).any()) and not bool(torch.isfinite(lse).any()) and not bool((lse == -torch.inf).any())
