@@ -950,8 +950,9 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   p.part_ml = reinterpret_cast<float*>(ws + 2 * y.wide + y.parts);
   p.split = reinterpret_cast<Split*>(p.part_ml + (size_t)2 * sms * 256 * 2);
   p.negate = a.scale_log2 < 0.f;
-  // (a scale of zero: all scores next to nothing, and what is not seen still at minus infinity)
-  p.scale = fmaxf(fabsf(a.scale_log2), 1e-30f);
+  // A scale of zero is the smallest number there is, 2^-149: its scores are below 2^-21 however large the products, and
+  // what is not seen stays at minus infinity.
+  p.scale = fmaxf(fabsf(a.scale_log2), 1.401298464e-45f);
   CUtensorMap qm, km, vm;
   const void *k = a.kv.k, *v = a.kv.v;
   uint64_t rows = (uint64_t)a.kv.n_pages * a.kv.n_kv_heads << a.kv.page_shift;

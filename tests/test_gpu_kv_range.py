@@ -38,3 +38,16 @@ def test_scores_beyond_32_bits(dtype, store, decode):
         refill(m, m.cache.k, m.cache.k_exp, m.keys, s, torch.ones((n, 2, 64), device="cuda"))
     out, lse = attend(m, decode, torch.ones_like(m.q), 1e37)                # scores of 64 * 1e37
     assert not bool(torch.isfinite(out).any()) and not bool(torch.isfinite(lse).any()) and not bool((lse == -torch.inf).any())
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("store", [BF16, E4M3])
+@pytest.mark.parametrize("scale", [0.0, 1e-38, -1e-36])
+def test_scales_next_to_nothing(decode, store, scale):
+    """Products of about 2^110 times a scale of about nothing."""
+    m = Made(67, [1, 3, 140], [1, 200, 140], heads=4, kv_heads=2, dim=64, store=store, page=64)
+    for s, n in enumerate(m.kv):
+        refill(m, m.cache.k, m.cache.k_exp, m.keys, s, (m.keys[s] * 2.0 ** 55).to(BF16))
+    q = (m.q.float() * 2.0 ** 55).to(BF16)
+    out, lse = attend(m, decode, q, scale)
+    check(out, lse, m.expected(q, scale, decode), BF16)
