@@ -500,7 +500,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
             }
             const uint32_t at = 64 * part + d;
             if (whole) {
-              const float inv = 1.f / sum;
+              const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (0: every score is minus infinity, and so is lse)
               T* out = static_cast<T*>(a.out) + (size_t)use.s * a.out_stride + (size_t)(h0 + 8 * nb + h) * D + at;
               *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
               if (a.lse && at == 0)
@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArg
     acc.z = __fmaf_rn(y.z, f, acc.z);
     acc.w = __fmaf_rn(y.w, f, acc.w);
   }
-  const float inv = 1.f / sum;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
   if (lse && d == 0) *lse = (top - kOffset + log2f(sum)) * 0.693147180559945309f;
 }

@@ -51,3 +51,41 @@ def test_scales_next_to_nothing(decode, store, scale):
     q = (m.q.float() * 2.0 ** 55).to(BF16)
     out, lse = attend(m, decode, q, scale)
     check(out, lse, m.expected(q, scale, decode), BF16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("decode", [False, True])
+def test_scores_of_minus_infinity(dtype, decode):
+    for none in (1, 40, 130, 200):
+        m = Made(61, [1, 3, 140], [1, 200, 140], heads=4, kv_heads=2, dim=64, dtype=dtype, page=64)
+        m.q[:, :, 7] = 0.5
+        for s, n in enumerate(m.kv):
+            k = m.keys[s].clone()
+            k[:none, :, 7] = -torch.inf
+            refill(m, m.cache.k, None, m.keys, s, k)
+        out, lse = attend(m, decode, m.q, 0.125)
+        row = 0
+        for s, (n, kv) in enumerate(zip(m.new, m.kv)):
+            for i in range(1 if decode else n):
+                seen = kv if decode else kv - n + i + 1
+                q = m.q[s if decode else row]
+                if seen <= none:
+                    assert bool((out[row] == 0).all()) and bool((lse[row] == -torch.inf).all()), (none, s, i)
+                else:
+                    k, v = m.keys[s][none:seen].repeat_interleave(2, 1), m.values[s][none:seen].repeat_interleave(2, 1)
+                    z = torch.einsum("hd,khd->hk", q.double(), k) * 0.125
+                    p = torch.softmax(z, 1)
+                    ref, sizes = torch.einsum("hk,khd->hd", p, v), torch.einsum("hk,khd->hd", p, v.abs())
+                    u = half_step(dtype)
+                    assert bool(((out[row].double() - ref).abs() <= sizes * (u + 2.0 ** -10) + ref.abs() * u + 2.0 ** -20).all())
+                row += 1
+
+
+@pytest.mark.parametrize("dtype,store", TYPES)
+@pytest.mark.parametrize("decode", [False, True])
+def test_scores_below_32_bits(dtype, store, decode):
+    m = Made(59, [1, 3, 140], [1, 200, 140], heads=4, kv_heads=2, dim=64, dtype=dtype, store=store, page=64)
+    for s, n in enumerate(m.kv):
+        refill(m, m.cache.k, m.cache.k_exp, m.keys, s, -torch.ones((n, 2, 64), device="cuda"))
+    out, lse = attend(m, decode, torch.ones_like(m.q), 1e37)
+    assert bool((out == 0).all()) and bool((lse == -torch.inf).all())
