@@ -25,7 +25,9 @@
 // rows leave an SM idle, and a block has at most two units in part, which a second, small kernel joins.  Warp 10 walks
 // the line ahead of the others, so the next unit's copies and first products run under the last one's end.
 //
-// e4m3 pages are first written out in 16 bits (exactly) into the workspace, once for all rows that read them.
+// e4m3 pages are first written out in bf16 (exactly) into the workspace, once for all rows that read them.  fp16 queries on
+// them: what a code stands for need not fit fp16, and q need not fit bf16; so q is taken as the sum of two bf16 numbers
+// (exactly) and P, too, is held as two: twice the products, 16 bits of P.
 //
 // Measured (32 query heads, 8 kv heads, head dim 128, bf16): 20,000 tokens 2.50 ms, 1,311 TFLOP/s of 1,679 that the library's
 // products reach at burst clocks (back to back, under the power cap, 2.93 ms); sixteen prompts of about 1,000 tokens 410 us,
@@ -45,13 +47,14 @@ constexpr int kEntries = 4;               // units that the roles of a block may
 constexpr int kUnit = 2;                  // what a unit costs besides its tiles, in tiles (with 1: 747 instead of 894 TFLOP/s on
                                           // sixteen prompts of about 1,000 tokens; with 3 and 4: 890 and 878)
 
-template <int D>
+template <int D, bool kTwo>
 struct Sizes {
   static constexpr int kPlanes = D / 64;
   static constexpr int kTile = kPlanes * kPlane;               // bytes of 128 rows of Q, K or V
-  static constexpr int kSlots = D == 128 ? 5 : 10;
+  static constexpr int kQ = kTwo ? 2 : 1;                      // tiles of Q for a tile of rows
+  static constexpr int kSlots = D == 64 ? 10 : kTwo ? 3 : 5;
   static constexpr int kBars = 2 * kSlots + 2 * kEntries + 13;
-  static constexpr int kBytes = 2 * kTile + kSlots * kTile + 8 * kBars;
+  static constexpr int kBytes = 2 * kQ * kTile + kSlots * kTile + 8 * kBars;
   static constexpr int kO = 256;                               // first TMEM column of O; S of tile i begins at 128 i
 };
 
@@ -392,16 +395,18 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   return r;
 }
 
-template <typename T, int D>
+// kTwo: rows are fp16, keys and values bf16; Q comes as two bf16 numbers whose sum it is, and P is held as two.
+template <typename T, int D, bool kTwo>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan p, const __grid_constant__ CUtensorMap q_map,
                const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-  using Z = Sizes<D>;
+  using Z = Sizes<D, kTwo>;
+  using M = typename std::conditional<kTwo, __nv_bfloat16, T>::type;     // type of the matrix instructions' operands
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ Work ring[kEntries];
   __shared__ uint32_t tmem_base, quit, clear_slot, clear_from;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const uint32_t q_a = smem_u32(smem), ring_a = q_a + 2 * Z::kTile;
+  const uint32_t q_a = smem_u32(smem), ring_a = q_a + 2 * Z::kQ * Z::kTile;
   const uint32_t full = ring_a + Z::kSlots * Z::kTile, empty = full + 8 * Z::kSlots, work_full = empty + 8 * Z::kSlots,
                  work_empty = work_full + 8 * kEntries, q_full = work_empty + 8 * kEntries, q_empty = q_full + 8,
                  s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 32, drained = o_full + 16,
@@ -513,7 +518,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
             }
           }
         }
-        const float off = m == -INFINITY ? 0.f : kShift<T> - m * c;
+        const float off = m == -INFINITY ? 0.f : kShift<M> - m * c;
         // P in halves of 64 keys: their products with V begin while the other half is computed
         f32x2 sum[4] = {0, 0, 0, 0};
         const f32x2 c2 = both(c, c), off2 = both(off, off);
@@ -522,16 +527,21 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
           if (k) read(1);
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
-            uint32_t pk[16];
+            uint32_t pk[16], low[kTwo ? 16 : 1];
 #pragma unroll
             for (int y = 0; y < 16; ++y) {
               float2 u = apart(fma2(both(__uint_as_float(x[32 * q + 2 * y]), __uint_as_float(x[32 * q + 2 * y + 1])), c2, off2));
               u.x = fast_exp2(u.x);
               u.y = fast_exp2(u.y);
               sum[y % 4] = add2(sum[y % 4], both(u.x, u.y));
-              pk[y] = pack2(u.x, u.y, T());
+              pk[y] = pack2(u.x, u.y, M());
+              if (kTwo) {
+                const float2 h = unpack2(pk[y], M());
+                low[y % (kTwo ? 16 : 1)] = pack2(u.x - h.x, u.y - h.y, M());
+              }
             }
-            tmem_st16(s_at + 32 * k + 16 * q, pk);
+            tmem_st16(s_at + (kTwo ? 64 : 32) * k + 16 * q, pk);
+            if (kTwo) tmem_st16(s_at + 64 * k + 32 + 16 * q, low);
           }
           tmem_wait_st();
           fence_before();
@@ -589,7 +599,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
 #pragma unroll
             for (int y = 0; y < 4; ++y) *reinterpret_cast<uint4*>(out + 32 * k + 8 * y) = v[y];
         }
-        if (mine && a.lse) a.lse[row * a.n_heads + head] = bad ? NAN : l == 0.f ? -INFINITY : (m * c - kShift<T> + log2f(l)) * 0.693147180559945309f;
+        if (mine && a.lse) a.lse[row * a.n_heads + head] = bad ? NAN : l == 0.f ? -INFINITY : (m * c - kShift<M> + log2f(l)) * 0.693147180559945309f;
         uint32_t again = __ballot_sync(0xffffffffu, mine && odd && !bad);
         for (; again; again &= again - 1) {
           const uint32_t b = __ffs(again) - 1;
@@ -649,14 +659,14 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
             if (!go) break;
             q_phase ^= 1;
             if (lane == 0) {
-              const uint32_t bytes = p.tq * a.group * 128 * Z::kPlanes;
+              const uint32_t bytes = p.tq * a.group * 128 * Z::kPlanes * Z::kQ;
               mbar_expect(q_full, (steps[0] ? bytes : 0) + (steps[1] ? bytes : 0));
               for (int i = 0; i < 2; ++i)
-                for (int c = 0; steps[i] && c < Z::kPlanes; ++c)
+                for (int c = 0; steps[i] && c < Z::kPlanes * Z::kQ; ++c)         // (the second numbers: total_new rows behind)
                   asm volatile(
                       "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                      ::"r"(q_a + i * Z::kTile + c * kPlane), "l"(reinterpret_cast<uint64_t>(&q_map)), "r"(c * 64),
-                      "r"((int)(w.h * a.group)), "r"(w.first + w.q0 + i * (int)p.tq), "r"(q_full) : "memory");
+                      ::"r"(q_a + i * Z::kQ * Z::kTile + c * kPlane), "l"(reinterpret_cast<uint64_t>(&q_map)), "r"(c % Z::kPlanes * 64),
+                      "r"((int)(w.h * a.group)), "r"(w.first + w.q0 + i * (int)p.tq + (c / Z::kPlanes ? (int)a.b.total_new : 0)), "r"(q_full) : "memory");
             }
           }
         }
@@ -674,15 +684,15 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       // At D = 64 the exponentials are the bound and a thread that issues a little later serves them better: the tiles
       // fall into turns (20,000 tokens: 733 against 694 TFLOP/s; at D = 128 it is 1,240 against 1,306).
       if (D == 64 ? lane == 0 : elect_one()) {
-        constexpr bool kBf = std::is_same<T, __nv_bfloat16>::value;
+        constexpr bool kBf = std::is_same<M, __nv_bfloat16>::value;
         const uint32_t s_shape = mma_shape(kKeys, kBf, p.negate != 0, false), o_shape = mma_shape(D, kBf, false, true);
         const uint32_t q_op = operand(q_a, 16), k_op = operand(ring_a, 16), v_op = operand(ring_a, kPlane);
         auto scores = [&](int i, uint32_t slot) {              // S_i = Q_i K^T
-          const uint32_t x = q_op + i * (Z::kTile >> 4), y = k_op + slot * (Z::kTile >> 4);
+          const uint32_t x = q_op + i * (Z::kQ * Z::kTile >> 4), y = k_op + slot * (Z::kTile >> 4);
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = ((k / 4) * kPlane + (k % 4) * 32) >> 4;
-            mma_ss(tmem + 128 * i, x + off, y + off, s_shape, k > 0);
+          for (int k = 0; k < Z::kQ * (D / 16); ++k) {
+            const uint32_t off = ((k / 4) * kPlane + (k % 4) * 32) >> 4, k_off = off % (Z::kTile >> 4);
+            mma_ss(tmem + 128 * i, x + off, y + k_off, s_shape, k > 0);
           }
           mma_commit(s_full + 8 * i);
         };
@@ -690,7 +700,10 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
           const uint32_t y = v_op + slot * (Z::kTile >> 4);
 #pragma unroll
           for (int k = 4 * half; k < 4 * half + 4; ++k)
-            mma_ts(tmem + Z::kO + D * i, tmem + 128 * i + 8 * k, y + (k * 2048 >> 4), o_shape, acc || k > 0);
+#pragma unroll
+            for (int n = 0; n < Z::kQ; ++n)
+              mma_ts(tmem + Z::kO + D * i, tmem + 128 * i + 8 * k + (kTwo ? 32 * (half + n) : 0), y + (k * 2048 >> 4), o_shape,
+                     acc || k > 0 || n > 0);
         };
         uint32_t slot = 0, phase = 0, q_phase = 0, c_phase = 0, p_phase[2] = {0, 0};
         auto take = [&] {                                      // the next slot, when it is there
@@ -798,7 +811,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         if (slot == kWhole) break;
         const uint32_t rest = (kKeys - from) * 8;              // 16-byte pieces of a plane
         for (uint32_t x = lane; x < rest * Z::kPlanes; x += 32)
-          *reinterpret_cast<uint4*>(smem + 2 * Z::kTile + slot * Z::kTile + x / rest * kPlane + from * 128 + x % rest * 16) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(smem + 2 * Z::kQ * Z::kTile + slot * Z::kTile + x / rest * kPlane + from * 128 + x % rest * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(cleared);
@@ -812,9 +825,10 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
 
 // Joins the parts of the units that several blocks hold: a block of this kernel takes eight rows, a warp each, of the unit
 // whose first part block x of the first kernel has.
-template <typename T, int D>
+template <typename T, int D, bool kTwo>
 __global__ void __launch_bounds__(256) prefill_join_kernel(const __grid_constant__ AttnArgs a, const Plan p) {
   constexpr int kPer = D / 32;
+  constexpr float kUp = kTwo ? 0.f : kShift<T>;
   const uint32_t lane = threadIdx.x % 32, c0 = blockIdx.x;
   wait_primary();
   const Work w = p.split[c0].w;           // (read beside `parts`, whatever that says)
@@ -853,15 +867,16 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const __grid_constant
     odd |= !(fabsf(f) < INFINITY) || !(fabsf(g) < INFINITY);
     *reinterpret_cast<uint32_t*>(out + y) = pack2(f, g, T());
   }
-  if (a.lse && lane == 0) a.lse[row * a.n_heads + head] = sum == 0.f ? -INFINITY : (top - kShift<T> + log2f(sum)) * 0.693147180559945309f;
+  if (a.lse && lane == 0) a.lse[row * a.n_heads + head] = sum == 0.f ? -INFINITY : (top - kUp + log2f(sum)) * 0.693147180559945309f;
   // (a sum that is NaN: a wrong page, or a score that is none)
   if (__any_sync(0xffffffffu, odd) && sum == sum)
     mend_row<T, D>(a, w.s, w.kv - w.n + t, w.tiles[i] * kKeys, w.kv, (uint32_t)row, head, lane);
 }
 
-// e4m3 pages as 16-bit rows [kv head][linear][D], a sequence after the other from multiples of 128 rows.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) widen_kernel(const AttnArgs a, const uint64_t linear, T* k_out, T* v_out) {
+// e4m3 pages as bf16 rows [kv head][linear][D], a sequence after the other from multiples of 128 rows.  Exact: a code has
+// four bits, and code * 2^e is between 2^-33 and bf16's largest value, but for 2^128, which the largest rows of bf16 may round to.
+template <int D>
+__global__ void __launch_bounds__(256) widen_kernel(const AttnArgs a, const uint64_t linear, __nv_bfloat16* k_out, __nv_bfloat16* v_out) {
   constexpr uint32_t kLanes = D / 8;
   __shared__ uint32_t seq, tile;
   const uint32_t lane = threadIdx.x % 32;
@@ -913,18 +928,37 @@ __global__ void __launch_bounds__(256) widen_kernel(const AttnArgs a, const uint
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 y = unpack_e4m3((i < 2 ? x.x : x.y) >> 16 * (i & 1) & 0xffffu);
-        u[i] = pack2(y.x * f, y.y * f, T());
+        u[i] = pack2(y.x * f, y.y * f, __nv_bfloat16());
       }
       *out = make_uint4(u[0], u[1], u[2], u[3]);
     }
   }
 }
 
+// fp16 rows of queries as two bf16 numbers whose sum they are: [2][rows][n_heads][D].
+__global__ void __launch_bounds__(256) split_kernel(const AttnArgs a, uint4* out) {
+  const uint32_t width = a.n_heads * a.head_dim / 8;           // 16-byte pieces of a row
+  const uint64_t n = (uint64_t)a.b.total_new * width, x = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x >= n) return;
+  const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const __half*>(a.q) + x / width * a.q_stride + x % width * 8);
+  const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = unpack2(in[i], __half());
+    hi[i] = pack2(f.x, f.y, __nv_bfloat16());
+    const float2 h = unpack2(hi[i], __nv_bfloat16());          // (infinities and NaN are in the first alone)
+    lo[i] = pack2(fabsf(f.x) < INFINITY ? f.x - h.x : 0.f, fabsf(f.y) < INFINITY ? f.y - h.y : 0.f, __nv_bfloat16());
+  }
+  out[x] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  out[n + x] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
 uint64_t round_up(uint64_t x, uint64_t n) { return (x + n - 1) / n * n; }
 
 struct Layout {
   Plan p;
-  uint64_t wide, parts, bytes;            // of the 16-bit copy of K (and V), of the parts' O, of all
+  uint64_t wide, two, parts, bytes;       // of the 16-bit copy of K (and V), of Q as two numbers, of the parts' O, of all
 };
 
 Layout layout(const AttnArgs& a, int sms) {
@@ -933,44 +967,57 @@ Layout layout(const AttnArgs& a, int sms) {
   if (a.store == GORGO_E4M3) {
     y.p.linear = round_up(a.total_kv, kKeys) + (uint64_t)kKeys * a.b.n_seqs;
     y.wide = round_up(y.p.linear * a.kv.n_kv_heads * a.head_dim * 2, 256);
+    if (a.type == GORGO_FP16) y.two = round_up((uint64_t)2 * a.b.total_new * a.n_heads * a.head_dim * 2, 256);
   }
   y.p.box = a.store == GORGO_E4M3 ? kKeys : (1u << a.kv.page_shift) < (uint32_t)kKeys ? 1u << a.kv.page_shift : kKeys;
   y.parts = (uint64_t)2 * sms * 256 * a.head_dim * 4;
-  y.bytes = 2 * y.wide + y.parts + (uint64_t)2 * sms * 256 * 8 + (uint64_t)sms * sizeof(Split);
+  y.bytes = 2 * y.wide + y.two + y.parts + (uint64_t)2 * sms * 256 * 8 + (uint64_t)sms * sizeof(Split);
   return y;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kTwo>
 cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
-  using Z = Sizes<D>;
+  using Z = Sizes<D, kTwo>;
   Layout y = layout(a, sms);
   Plan& p = y.p;
   unsigned char* ws = static_cast<unsigned char*>(a.workspace);
-  p.part_o = reinterpret_cast<float*>(ws + 2 * y.wide);
-  p.part_ml = reinterpret_cast<float*>(ws + 2 * y.wide + y.parts);
+  p.part_o = reinterpret_cast<float*>(ws + 2 * y.wide + y.two);
+  p.part_ml = reinterpret_cast<float*>(ws + 2 * y.wide + y.two + y.parts);
   p.split = reinterpret_cast<Split*>(p.part_ml + (size_t)2 * sms * 256 * 2);
   p.negate = a.scale_log2 < 0.f;
   // A scale of zero is the smallest number there is, 2^-149: its scores are below 2^-21 however large the products, and
   // what is not seen stays at minus infinity.
   p.scale = fmaxf(fabsf(a.scale_log2), 1.401298464e-45f);
   CUtensorMap qm, km, vm;
-  const void *k = a.kv.k, *v = a.kv.v;
+  const void *q = a.q, *k = a.kv.k, *v = a.kv.v;
+  uint64_t q_rows = a.b.total_new, q_stride = a.q_stride;
+  const uint32_t type = kTwo ? (uint32_t)GORGO_BF16 : a.type;
   uint64_t rows = (uint64_t)a.kv.n_pages * a.kv.n_kv_heads << a.kv.page_shift;
   if (p.linear) {
     k = ws;
     v = ws + y.wide;
     rows = p.linear * a.kv.n_kv_heads;
     const uint64_t tiles = p.linear / kKeys;
-    widen_kernel<T, D><<<dim3((uint32_t)tiles, a.kv.n_kv_heads), 256, 0, st>>>(a, p.linear, reinterpret_cast<T*>(ws), reinterpret_cast<T*>(ws + y.wide));
+    widen_kernel<D><<<dim3((uint32_t)tiles, a.kv.n_kv_heads), 256, 0, st>>>(a, p.linear, reinterpret_cast<__nv_bfloat16*>(ws),
+                                                                            reinterpret_cast<__nv_bfloat16*>(ws + y.wide));
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  if (!make_rows_map(&qm, a.q, a.b.total_new, a.n_heads, D, a.q_stride, a.type, p.tq, a.group) ||
-      !make_pool_map(&km, k, rows, D, a.type, p.box, 1) || !make_pool_map(&vm, v, rows, D, a.type, p.box, 1))
+  if (kTwo) {
+    q = ws + 2 * y.wide;
+    q_rows *= 2;
+    q_stride = (uint64_t)a.n_heads * D;
+    const uint64_t pieces = a.b.total_new * q_stride / 8;
+    split_kernel<<<(uint32_t)((pieces + 255) / 256), 256, 0, st>>>(a, reinterpret_cast<uint4*>(ws + 2 * y.wide));
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  if (!make_rows_map(&qm, q, (uint32_t)q_rows, a.n_heads, D, q_stride, type, p.tq, a.group) ||
+      !make_pool_map(&km, k, rows, D, type, p.box, 1) || !make_pool_map(&vm, v, rows, D, type, p.box, 1))
     return cudaErrorUnknown;
-  cudaError_t e = allow_smem<prefill_kernel<T, D>>(Z::kBytes);
+  cudaError_t e = allow_smem<prefill_kernel<T, D, kTwo>>(Z::kBytes);
   if (e != cudaSuccess) return e;
-  prefill_kernel<T, D><<<sms, kThreads, Z::kBytes, st>>>(a, p, qm, km, vm);
+  prefill_kernel<T, D, kTwo><<<sms, kThreads, Z::kBytes, st>>>(a, p, qm, km, vm);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(sms, 32);
@@ -981,7 +1028,13 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   early.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, prefill_join_kernel<T, D>, a, p);
+  return cudaLaunchKernelEx(&cfg, prefill_join_kernel<T, D, kTwo>, a, p);
+}
+
+template <int D>
+cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
+  if (a.type == GORGO_BF16) return launch<__nv_bfloat16, D, false>(a, sms, st);
+  return a.store == GORGO_E4M3 ? launch<__half, D, true>(a, sms, st) : launch<__half, D, false>(a, sms, st);
 }
 
 }  // namespace
@@ -993,8 +1046,7 @@ bool prefill_fits(const AttnArgs& a) {
 uint64_t prefill_workspace(const AttnArgs& a, int sms) { return a.b.total_new ? layout(a, sms).bytes : 0; }
 
 cudaError_t launch_attn_prefill(const AttnArgs& a, int sms, cudaStream_t st) {
-  if (a.type == GORGO_BF16) return a.head_dim == 128 ? launch<__nv_bfloat16, 128>(a, sms, st) : launch<__nv_bfloat16, 64>(a, sms, st);
-  return a.head_dim == 128 ? launch<__half, 128>(a, sms, st) : launch<__half, 64>(a, sms, st);
+  return a.head_dim == 128 ? launch<128>(a, sms, st) : launch<64>(a, sms, st);
 }
 
 }  // namespace gorgo

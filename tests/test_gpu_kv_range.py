@@ -89,3 +89,38 @@ def test_scores_below_32_bits(dtype, store, decode):
         refill(m, m.cache.k, m.cache.k_exp, m.keys, s, -torch.ones((n, 2, 64), device="cuda"))
     out, lse = attend(m, decode, torch.ones_like(m.q), 1e37)
     assert bool((out == 0).all()) and bool((lse == -torch.inf).all())
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("k_size,v_size,scale", [(2.0 ** 17, 1.0, 2.0 ** -20), (1.0, 2.0 ** 12, 0.125),
+                                                  (2.0 ** -18, 1.0, 2.0 ** 14), (1.0, 2.0 ** -14, 0.125)])
+def test_fp16_rows_on_codes_beyond_fp16(decode, dim, k_size, v_size, scale):
+    """Codes of a cache that was filled from bf16: what they stand for need not fit fp16, the result does."""
+    m = Made(71, [1, 3, 140], [1, 200, 140], heads=4, kv_heads=2, dim=dim, dtype=FP16, store=E4M3, page=64)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for s, n in enumerate(m.kv):
+        refill(m, m.cache.k, m.cache.k_exp, m.keys, s, m.keys[s] * k_size)
+        big = 1.0 + 15.0 * (torch.rand((n, 1, 1), generator=g, device="cuda") < 0.1) if v_size > 1 and n > 1 else 1.0
+        refill(m, m.cache.v, m.cache.v_exp, m.values, s, m.values[s] * v_size * big)
+    out, lse = attend(m, decode, m.q, scale)
+    want = m.expected(m.q, scale, decode)
+    want[2] += 2.0 ** -25                                    # a result below fp16's normal range: half a step of 2^-24
+    fits = want[0].abs().amax((1, 2)) < 65000                # (rows of few keys may not)
+    assert int(fits.sum()) >= fits.numel() // 2
+    check(out[fits], lse[fits], [w[fits] for w in want], FP16)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_the_largest_fp16_value_in_a_row_of_codes(decode):
+    m = Made(73, [140], [140], heads=4, kv_heads=2, dim=64, dtype=FP16, store=E4M3, page=64)
+    v = m.values[0].clone()
+    v[3, :, 9] = 65504.0                                     # rounds to a code that stands for 65,536
+    refill(m, m.cache.v, m.cache.v_exp, m.values, 0, v)
+    q = m.q * 0.1
+    q[:20] = 0                                               # (rows of few keys: their share of it fits)
+    out, lse = attend(m, decode, q, 0.125)
+    want = m.expected(q, 0.125, decode)
+    fits = want[0].abs().amax((1, 2)) < 65000
+    assert int(fits.sum()) >= fits.numel() // 2
+    check(out[fits], lse[fits], [w[fits] for w in want], FP16)
