@@ -17,7 +17,9 @@
 // that it is not what limits the result; the tensor pipe is nearly idle here.
 //
 // e4m3 pages: codes become fp16, exactly; q as fp16 after a power of two per head that makes its largest value about
-// 2^10 (exact but for what is 2^-34 of it); the keys' powers of two multiply the scores, the values' are added to the exponents of P.
+// 2^10 (exact but for what is 2^-34 of it); the keys' powers of two multiply the scores, the values' are added to the exponents
+// of P.  Those powers may be 2^144 apart, so for l the exponentials are taken 2^30 larger, and a factor between maxima is applied
+// to l as two square roots: neither loses a key that counts.
 //
 // Measured (32 query heads, 8 kv heads, head dim 128): 16 sequences of about 20,000 tokens in bf16, 1.47 GB, 227 us: 6.5 TB/s;
 // 64 in e4m3, 3.6 GB, 640 us: 5.7 TB/s; four of about 1,000: 12.4 us in a graph, latency.
@@ -30,6 +32,22 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr float kOffset = 14.f;           // p = 2^(z - m + kOffset): fp16 keeps p down to 2^-38 of the largest
+constexpr int kLift = 30;                 // e4m3: powers of two that l holds more than p
+
+// l and o of a run whose maximum `m` becomes `top`: l * 2^(m - top) for e4m3 pages, where the difference may be large although
+// the run counts, and 2^(m - top), the factor of o.
+template <bool kQuant>
+__device__ __forceinline__ float move_max(float m, float top, float& l) {
+  if (m == top) return 1.f;
+  if (!kQuant) {
+    const float f = fast_exp2(m - top);
+    l *= f;
+    return f;
+  }
+  const float h = fast_exp2(0.5f * (m - top));
+  l = l * h * h;
+  return h * h;
+}
 
 template <bool kQuant, int D, int NB>
 struct Sizes {
@@ -372,9 +390,8 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const float x = fmaxf(m[nb][i], top[nb][i]);
-            f[i] = x == m[nb][i] ? 1.f : fast_exp2(m[nb][i] - x);
+            f[i] = move_max<kQuant>(m[nb][i], x, l[nb][i]);
             m[nb][i] = x;
-            l[nb][i] *= f[i];
           }
 #pragma unroll
           for (int k = 0; k < kSteps; ++k)
@@ -385,14 +402,19 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
       uint32_t ph[kBlocks][NB][2], pl[kBlocks][NB][2];   // P as the second operand (k = key, n = head), high and low part
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const float m0 = m[nb][0] == -INFINITY ? 0.f : m[nb][0] - kOffset, m1 = m[nb][1] == -INFINITY ? 0.f : m[nb][1] - kOffset;
+        constexpr float kUp = kOffset + (kQuant ? kLift : 0);
+        const float m0 = m[nb][0] == -INFINITY ? 0.f : m[nb][0] - kUp, m1 = m[nb][1] == -INFINITY ? 0.f : m[nb][1] - kUp;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {   // key g + 8 i
-            const float x = fast_exp2(c[b][nb][2 * i] - m0), y = fast_exp2(c[b][nb][2 * i + 1] - m1);
+            float x = fast_exp2(c[b][nb][2 * i] - m0), y = fast_exp2(c[b][nb][2 * i + 1] - m1);
             l[nb][0] = __fmaf_rn(x, vi[b][i], l[nb][0]);
             l[nb][1] = __fmaf_rn(y, vi[b][i], l[nb][1]);
+            if (kQuant) {
+              x *= pow2i(-kLift);
+              y *= pow2i(-kLift);
+            }
             const uint32_t hi = pack2(x, y, M());
             ph[b][nb][i] = transpose8(hi);
             if (kLow) {
@@ -464,6 +486,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
           x += __shfl_xor_sync(0xffffffffu, x, 4);
           x += __shfl_xor_sync(0xffffffffu, x, 8);
           x += __shfl_xor_sync(0xffffffffu, x, 16);
+          if (kQuant) x *= pow2i(-kLift);
           if (bad || !alive) x = NAN;
           if (g == 0) {
             ml[(warp * 8 + 2 * t + i) * 2] = m[nb][i];
@@ -490,9 +513,10 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-              const float mw = ml[(w * 8 + h) * 2], f = mw == top ? 1.f : fast_exp2(mw - top);
+              float lw = ml[(w * 8 + h) * 2 + 1];
+              const float f = move_max<kQuant>(ml[(w * 8 + h) * 2], top, lw);
               const float4 y = *reinterpret_cast<const float4*>(merge + (w * 8 + h) * Z::kPad + d);
-              sum = __fmaf_rn(ml[(w * 8 + h) * 2 + 1], f, sum);
+              sum += lw;
               acc.x = __fmaf_rn(y.x, f, acc.x);
               acc.y = __fmaf_rn(y.y, f, acc.y);
               acc.z = __fmaf_rn(y.z, f, acc.z);
@@ -526,7 +550,7 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
 // first kernel has.  Its threads take every 8th or 16th part, 16 bytes of the row each, with a running maximum, so that
 // parts arrive side by side.
 constexpr int kJoinThreads = 256;
-template <typename T, int D, int NB>
+template <typename T, bool kQuant, int D, int NB>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArgs a, const Split sp) {
   constexpr uint32_t kH = 8 * NB, kVec = D / 4, kWays = kJoinThreads / kVec;
   const uint32_t way = threadIdx.x / kVec, d = threadIdx.x % kVec * 4, h = blockIdx.y;
@@ -545,12 +569,12 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArg
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
   for (uint32_t c = c0 + way; c <= c1; c += kWays) {
-    const float2 p = *reinterpret_cast<const float2*>(sp.part_ml + at(c) * 2);
+    float2 p = *reinterpret_cast<const float2*>(sp.part_ml + at(c) * 2);
     const float4 y = *reinterpret_cast<const float4*>(sp.part_o + at(c) * D + d);
     const float now = fmaxf(top, p.x);
-    const float f = top == now ? 1.f : fast_exp2(top - now), w = p.x == now ? 1.f : fast_exp2(p.x - now);
+    const float f = move_max<kQuant>(top, now, sum), w = move_max<kQuant>(p.x, now, p.y);
     top = now;
-    sum = __fmaf_rn(p.y, w, sum * f);
+    sum += p.y;
     acc.x = __fmaf_rn(y.x, w, acc.x * f);
     acc.y = __fmaf_rn(y.y, w, acc.y * f);
     acc.z = __fmaf_rn(y.z, w, acc.z * f);
@@ -566,9 +590,10 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const AttnArg
   acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (uint32_t w = 0; w < kWays; ++w) {
-    const float f = part[w][D] == top ? 1.f : fast_exp2(part[w][D] - top);
+    float lw = part[w][D + 1];
+    const float f = move_max<kQuant>(part[w][D], top, lw);
     const float4 y = *reinterpret_cast<const float4*>(&part[w][d]);
-    sum = __fmaf_rn(part[w][D + 1], f, sum);
+    sum += lw;
     acc.x = __fmaf_rn(y.x, f, acc.x);
     acc.y = __fmaf_rn(y.y, f, acc.y);
     acc.z = __fmaf_rn(y.z, f, acc.z);
@@ -613,7 +638,7 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   early.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, D, NB>, a, sp);
+  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, kQuant, D, NB>, a, sp);
 }
 
 template <typename T, bool kQuant, int D>

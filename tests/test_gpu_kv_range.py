@@ -124,3 +124,18 @@ def test_the_largest_fp16_value_in_a_row_of_codes(decode):
     fits = want[0].abs().amax((1, 2)) < 65000
     assert int(fits.sum()) >= fits.numel() // 2
     check(out[fits], lse[fits], [w[fits] for w in want], FP16)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_values_far_apart_in_size(decode):
+    """Rows of zeros beside one of about 2^125, all scores zero: each key counts the same."""
+    for kv in (2, 40, 300, 9000):
+        for at in (0, kv // 2, kv - 1):
+            m = Made(79, [1], [kv], heads=4, kv_heads=2, dim=64, store=E4M3, page=64)
+            v = torch.zeros((kv, 2, 64), dtype=torch.float64, device="cuda")
+            v[at] = 2.0 ** 125
+            refill(m, m.cache.v, m.cache.v_exp, m.values, 0, v)
+            out, lse = attend(m, decode, m.q * 0, 0.125)
+            want = v[at, 0, 0] / kv
+            assert bool(((out.double() - want).abs() <= want * (2 * 2.0 ** -8 + 2.0 ** -10)).all()), (kv, at)
+            assert bool(((lse.double() - torch.log(torch.tensor(float(kv)))).abs() < 1e-4).all())
