@@ -57,7 +57,7 @@ __device__ __noinline__ void attend_row(const AttnArgs& a, uint32_t s, int seen,
     z *= a.scale_log2;
     load_row<T, D>(a.kv.v, a.kv.v_exp, at, lane, k);
     const float top = fmaxf(m, z);
-    const float keep = top == -INFINITY ? 1.f : exp2f(m - top), p = top == -INFINITY ? 0.f : exp2f(z - top);
+    const float keep = m == top ? 1.f : exp2f(m - top), p = z == -INFINITY ? 0.f : exp2f(z - top);   // (a NaN in z stays)
     l = __fmaf_rn(l, keep, p);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) o[i] = __fmaf_rn(o[i], keep, p * k[i]);
