@@ -18,7 +18,8 @@
 //
 // Values behind the last key of a sequence may be anything: they are overwritten with zeros in shared memory.  A value
 // that is not finite and that a row of its tile does not see would reach the row as 0 * x: rows whose result is not
-// finite look at the values behind their own last key, and are computed again key by key if one of those is the cause.
+// finite are listed (a byte a row and head), and the second kernel, in which nothing waits for another warp, looks at the
+// values behind their own last key and computes them again key by key if one of those is the cause (one row of 100,000 keys: 34 ms; 18,900 rows of 30,000: 108 ms).
 //
 // All (sequence, kv head, tokens) units with their tiles of keys, and two places more for what a unit costs besides, are
 // laid out as one line that is cut into as many equal pieces as SMs: no batch, no lengths and no long prefix under a few
@@ -67,6 +68,8 @@ struct Plan {
   float* part_o;                          // [2 * grid][256][D]
   float* part_ml;                         // [2 * grid][256][2]
   struct Split* split;                    // [grid]
+  uint8_t* again;                         // [total_new][n_heads]: 1: the row's result is not finite and it has to be looked at
+  uint32_t* odd;                          // [grid]: whether a block has such rows
 };
 
 struct Work {                             // a unit, or a block's part of it
@@ -404,7 +407,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   using M = typename std::conditional<kTwo, __nv_bfloat16, T>::type;     // type of the matrix instructions' operands
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ Work ring[kEntries];
-  __shared__ uint32_t tmem_base, quit, clear_slot, clear_from;
+  __shared__ uint32_t tmem_base, quit, clear_slot, clear_from, any_odd;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t q_a = smem_u32(smem), ring_a = q_a + 2 * Z::kQ * Z::kTile;
   const uint32_t full = ring_a + Z::kSlots * Z::kTile, empty = full + 8 * Z::kSlots, work_full = empty + 8 * Z::kSlots,
@@ -413,7 +416,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
                  clear = drained + 8, cleared = clear + 8;
 
   if (threadIdx.x == 0) {
-    quit = 0;
+    quit = any_odd = 0;
     for (int i = 0; i < Z::kSlots; ++i) {
       mbar_init(full + 8 * i, 1);
       mbar_init(empty + 8 * i, 1);
@@ -557,6 +560,8 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       }
       const bool bad = pos >= w.none_from || !go;
       if (w.slot != kWhole) {
+        // (the second kernel sees these rows' results first)
+        if (mine && lo == 0) p.again[(size_t)(w.first + t) * a.n_heads + w.h * a.group + in_group] = 0;
         const size_t part = (size_t)w.slot * 256 + i * 128 + r;
         *reinterpret_cast<float2*>(p.part_ml + 2 * part) = make_float2(m * c, bad ? NAN : l);
 #pragma unroll
@@ -600,12 +605,10 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
             for (int y = 0; y < 4; ++y) *reinterpret_cast<uint4*>(out + 32 * k + 8 * y) = v[y];
         }
         if (mine && a.lse) a.lse[row * a.n_heads + head] = bad ? NAN : l == 0.f ? -INFINITY : (m * c - kShift<M> + log2f(l)) * 0.693147180559945309f;
-        uint32_t again = __ballot_sync(0xffffffffu, mine && odd && !bad);
-        for (; again; again &= again - 1) {
-          const uint32_t b = __ffs(again) - 1;
-          mend_row<T, D>(a, w.s, __shfl_sync(0xffffffffu, pos, b), w.tiles[i] * kKeys, w.kv, (uint32_t)__shfl_sync(0xffffffffu, (int)row, b),
-                         __shfl_sync(0xffffffffu, head, b), lane);
-        }
+        // (a sum that is not finite: the scores are the cause)
+        odd = mine && odd && l < INFINITY;
+        if (mine) p.again[row * a.n_heads + head] = odd;
+        if (odd) any_odd = 1;
       }
       fence_before();
       __syncwarp();
@@ -821,16 +824,52 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   __syncthreads();
   fence_after();
   if (warp == 9) tmem_free(tmem, 512);
+  if (threadIdx.x == 0) p.odd[blockIdx.x] = any_odd;
+}
+
+// Keys that the tile of rows of a sequence's new token t took.
+__device__ __forceinline__ int keys_taken(int t, int tq, int n, int kv) {
+  const int last = kv - n + min((t / tq + 1) * tq, n) - 1;
+  return last < 0 ? 0 : min((last / kKeys + 1) * kKeys, kv);
+}
+
+// By all warps of the blocks y < kListBlocks of the second kernel: rows on the list.  Neighbours go to different warps: they
+// are long.
+constexpr uint32_t kListBlocks = 4;
+template <typename T, int D>
+__device__ __noinline__ void mend_list(const AttnArgs& a, const Plan& p, uint32_t lane) {
+  const uint64_t rows = (uint64_t)a.b.total_new * a.n_heads, warps = (uint64_t)gridDim.x * kListBlocks * 8;
+  const uint64_t me = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 8 + threadIdx.x / 32;
+  for (uint64_t x0 = 0; x0 * warps + me < rows; x0 += 32) {
+    const uint64_t mine = (x0 + lane) * warps + me;
+    uint32_t left = __ballot_sync(0xffffffffu, mine < rows && p.again[mine < rows ? mine : 0] == 1);
+    for (; left; left &= left - 1) {
+      const uint64_t x = (x0 + __ffs(left) - 1) * warps + me;
+      const uint32_t row = (uint32_t)(x / a.n_heads);
+      if ((int)row >= a.b.cu_new[a.b.n_seqs]) continue;        // (nobody's rows are not on the list: what is there is left over)
+      const uint32_t s = warp_find_seq(a.b, row, lane);
+      const SeqPlace q = seq_place(a, s);
+      const int t = (int)row - q.first, pos = q.kv - q.n + t;
+      if (q.bad || t < 0 || t >= q.n || pos < 0) continue;
+      mend_row<T, D>(a, s, pos / kKeys * kKeys, pos, keys_taken(t, p.tq, q.n, q.kv), row, (uint32_t)(x % a.n_heads), lane);
+    }
+  }
 }
 
 // Joins the parts of the units that several blocks hold: a block of this kernel takes eight rows, a warp each, of the unit
-// whose first part block x of the first kernel has.
+// whose first part block x of the first kernel has.  Before that some blocks see to the rows on the list, if there are any.
 template <typename T, int D, bool kTwo>
-__global__ void __launch_bounds__(256) prefill_join_kernel(const __grid_constant__ AttnArgs a, const Plan p) {
+__global__ void __launch_bounds__(256, 6)
+prefill_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan p) {
   constexpr int kPer = D / 32;
   constexpr float kUp = kTwo ? 0.f : kShift<T>;
   const uint32_t lane = threadIdx.x % 32, c0 = blockIdx.x;
   wait_primary();
+  if (blockIdx.y < kListBlocks) {
+    uint32_t odd_rows = 0;
+    for (uint32_t x = lane; x < gridDim.x; x += 32) odd_rows |= p.odd[x];
+    if (__any_sync(0xffffffffu, odd_rows != 0)) mend_list<T, D>(a, p, lane);
+  }
   const Work w = p.split[c0].w;           // (read beside `parts`, whatever that says)
   const uint32_t parts = p.split[c0].parts;
   if (parts == 0) return;
@@ -869,8 +908,9 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const __grid_constant
   }
   if (a.lse && lane == 0) a.lse[row * a.n_heads + head] = sum == 0.f ? -INFINITY : (top - kUp + log2f(sum)) * 0.693147180559945309f;
   // (a sum that is NaN: a wrong page, or a score that is none)
-  if (__any_sync(0xffffffffu, odd) && sum == sum)
-    mend_row<T, D>(a, w.s, w.kv - w.n + t, w.tiles[i] * kKeys, w.kv, (uint32_t)row, head, lane);
+  const int pos = w.kv - w.n + t;
+  if (__any_sync(0xffffffffu, odd) && sum < INFINITY && pos >= 0)
+    mend_row<T, D>(a, w.s, pos / kKeys * kKeys, pos, keys_taken(t, p.tq, w.n, w.kv), (uint32_t)row, head, lane);
 }
 
 // e4m3 pages as bf16 rows [kv head][linear][D], a sequence after the other from multiples of 128 rows.  Exact: a code has
@@ -971,7 +1011,8 @@ Layout layout(const AttnArgs& a, int sms) {
   }
   y.p.box = a.store == GORGO_E4M3 ? kKeys : (1u << a.kv.page_shift) < (uint32_t)kKeys ? 1u << a.kv.page_shift : kKeys;
   y.parts = (uint64_t)2 * sms * 256 * a.head_dim * 4;
-  y.bytes = 2 * y.wide + y.two + y.parts + (uint64_t)2 * sms * 256 * 8 + (uint64_t)sms * sizeof(Split);
+  y.bytes = 2 * y.wide + y.two + y.parts + (uint64_t)2 * sms * 256 * 8 + round_up((uint64_t)sms * sizeof(Split), 256) +
+            round_up((uint64_t)sms * 4, 256) + round_up((uint64_t)a.b.total_new * a.n_heads, 256);
   return y;
 }
 
@@ -984,6 +1025,8 @@ cudaError_t launch(const AttnArgs& a, int sms, cudaStream_t st) {
   p.part_o = reinterpret_cast<float*>(ws + 2 * y.wide + y.two);
   p.part_ml = reinterpret_cast<float*>(ws + 2 * y.wide + y.two + y.parts);
   p.split = reinterpret_cast<Split*>(p.part_ml + (size_t)2 * sms * 256 * 2);
+  p.odd = reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(p.split) + round_up((uint64_t)sms * sizeof(Split), 256));
+  p.again = reinterpret_cast<uint8_t*>(p.odd) + round_up((uint64_t)sms * 4, 256);
   p.negate = a.scale_log2 < 0.f;
   // A scale of zero is the smallest number there is, 2^-149: its scores are below 2^-21 however large the products, and
   // what is not seen stays at minus infinity.

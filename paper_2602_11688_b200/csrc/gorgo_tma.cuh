@@ -52,8 +52,8 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// Clock ticks after which a wait gives up: about ten seconds, many times what a unit of work takes, rows that are
-// computed again among it.
+// Clock ticks after which a wait gives up: about ten seconds, many times what a unit of work takes (2^24 keys in prefill:
+// 131,072 steps of 3,300 ticks, 0.25 s).
 constexpr long long kWaitTicks = 20000000000ll;
 static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
   const long long from = clock64();
