@@ -110,16 +110,14 @@ __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
 // New tokens and all tokens of sequence s; a wrong length is reported and counts as no tokens.
 struct SeqLen {
   int first, n, kv;                       // first row, new tokens, tokens in all
-  bool ok;
+  bool placed, ok;                        // its place in the packed array makes sense; so does its length
 };
 __device__ __forceinline__ bool kv_len_ok(const BatchView& b, int kv) { return kv >= 0 && (uint32_t)kv <= b.max_kv; }
 __device__ __forceinline__ SeqLen seq_len(const BatchView& b, uint32_t s) {
   const int a = b.cu_new[s], e = b.cu_new[s + 1], kv = b.kv_len[s];
-  SeqLen r = {a, e - a, kv, true};
-  if (a < 0 || e < a || (uint32_t)e > b.total_new || !kv_len_ok(b, kv)) {
-    report(b.status, GORGO_KV_BAD_LENGTH);
-    r.ok = false;
-  }
+  SeqLen r = {a, e - a, kv, a >= 0 && e >= a && (uint32_t)e <= b.total_new, false};
+  r.ok = r.placed && kv_len_ok(b, kv);
+  if (!r.ok) report(b.status, GORGO_KV_BAD_LENGTH);
   return r;
 }
 

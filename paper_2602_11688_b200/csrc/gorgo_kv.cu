@@ -16,7 +16,7 @@ constexpr int kMoveThreads = 256;
 constexpr int kMaxTok = 32;               // tokens of a block at most: a lane finds each one's place
 
 // By the first warp: where the tokens first, first + 1, ... lie: the pool row of their kv head 0; -1: the token belongs to no
-// sequence; -2: to one, but has no place.
+// sequence, or to one whose place in the packed array makes no sense; -2: to one, but has no place.
 __device__ __forceinline__ void find_places(const KvView& kv, const BatchView& b, uint32_t first, uint32_t n_tok,
                                             int64_t* place) {
   if (threadIdx.x >= 32) return;
@@ -36,7 +36,7 @@ __device__ __forceinline__ void find_places(const KvView& kv, const BatchView& b
       row = pool_row(kv, b, s, 0, (uint32_t)j);
       if (row < 0) report(b.status, GORGO_KV_BAD_PAGE);
     }
-    if (row < 0) row = -2;
+    if (row < 0 && q.placed) row = -2;
   }
   place[lane] = row;
 }

@@ -52,3 +52,49 @@ def test_rows_that_see_a_wrong_page_and_rows_before_it(store):
             assert bool(torch.isnan(out[first:300]).all())
             keep = list(range(first)) + list(range(300, 340))
             check(out[keep], None, [w[keep] for w in want], BF16)
+
+
+def test_read_leaves_rows_without_a_place():
+    from paper_2602_11688_b200 import binding as gb
+    m = Made(89, [3, 4, 2], [30, 70, 40], page=16)
+    m.batch.cu_new[2] = 100
+    out = [torch.full((9, 2, 64), 7.0, dtype=BF16, device="cuda") for _ in "kv"]
+    m.cache.read(m.batch, out=tuple(out))
+    assert int(m.batch.status.item()) == gb.GORGO_KV_BAD_LENGTH
+    for o, kept in zip(out, (m.keys, m.values)):
+        assert torch.equal(o[:3], kept[0][-3:].to(BF16)) and bool((o[3:] == 7).all())
+
+
+def test_prefill_leaves_rows_without_a_place():
+    from paper_2602_11688_b200 import binding as gb
+    m = Made(89, [3, 4, 2], [30, 70, 40], page=16)
+    m.batch.cu_new[2] = 100
+    want = m.expected(m.q, 0.125, False)
+    out = torch.full((9, 4, 64), 7.0, dtype=BF16, device="cuda")
+    m.cache.prefill(m.batch, m.q, out=out)
+    assert int(m.batch.status.item()) == gb.GORGO_KV_BAD_LENGTH
+    check(out[:3], None, [w[:3] for w in want], BF16)
+    assert bool((out[3:] == 7).all())
+
+
+def test_write_touches_nothing_for_rows_without_a_place():
+    for fault in ("beyond", "decreasing", "short"):
+        m = Made(89, [3, 4, 2], [30, 70, 40], page=16)
+        if fault == "beyond":
+            m.batch.cu_new[2] = 100                          # rows 0 to 2 are the first sequence's, the others nobody's
+        elif fault == "decreasing":
+            m.batch.cu_new[2] = 2
+        else:
+            m.batch.kv_len[1] = 3                            # four new tokens of three: the first has no position
+        x = torch.ones((9, 2, 64), dtype=BF16, device="cuda")
+        before = m.cache.k.clone()
+        m.cache.write(m.batch, x, x)
+        assert int(m.batch.status.item()) == 2
+        changed = (m.cache.k.view(torch.int16) != before.view(torch.int16)).any(-1)
+        allowed = torch.zeros_like(changed)
+        for s, lo, hi in ((0, 27, 30),) + {"beyond": (), "decreasing": ((2, 33, 40),), "short": ((1, 0, 3), (2, 38, 40))}[fault]:
+            pg, slot = m.where(s, torch.arange(lo, hi, device="cuda"))
+            allowed[pg, :, slot] = True
+        assert not bool((changed & ~allowed).any())
+        pg, slot = m.where(0, torch.arange(27, 29 if fault == "decreasing" else 30, device="cuda"))   # (row 2 is two sequences' there)
+        assert bool((m.cache.k[pg, :, slot] == 1).all())
