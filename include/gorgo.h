@@ -501,7 +501,8 @@ const char *gorgo_strerror(int code);
 enum { GORGO_BF16 = 0, GORGO_FP16 = 1, GORGO_E4M3 = 2 };
 enum {
   GORGO_KV_BAD_PAGE = 1,              /* a table entry that is needed is outside [0, n_pages)       */
-  GORGO_KV_BAD_LENGTH = 2,            /* cu_new or kv_len decreasing, negative or above its bound   */
+  GORGO_KV_BAD_LENGTH = 2,            /* cu_new or kv_len decreasing, negative or above its bound,  */
+                                      /* more new tokens than max_new (all but decode)              */
   GORGO_KV_WAIT_LIMIT = 4             /* a bounded wait inside a kernel ran out                     */
 };
 

@@ -27,7 +27,7 @@ struct BatchView {
   const int32_t* kv_len;
   const int32_t* table;
   uint32_t* status;
-  uint32_t n_seqs, total_new, max_kv, table_stride;
+  uint32_t n_seqs, total_new, max_new, max_kv, table_stride;
 };
 
 // Launchers; every size has been checked by the caller.
@@ -108,6 +108,10 @@ __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
 }
 
 // New tokens and all tokens of sequence s; a wrong length is reported and counts as no tokens.
+// (a, e: cu_new of a sequence and of the one behind it)
+__device__ __forceinline__ bool placed_ok(const BatchView& b, int a, int e) {
+  return a >= 0 && e >= a && (uint32_t)e <= b.total_new && (uint32_t)(e - a) <= b.max_new;
+}
 struct SeqLen {
   int first, n, kv;                       // first row, new tokens, tokens in all
   bool placed, ok;                        // its place in the packed array makes sense; so does its length
@@ -115,7 +119,7 @@ struct SeqLen {
 __device__ __forceinline__ bool kv_len_ok(const BatchView& b, int kv) { return kv >= 0 && (uint32_t)kv <= b.max_kv; }
 __device__ __forceinline__ SeqLen seq_len(const BatchView& b, uint32_t s) {
   const int a = b.cu_new[s], e = b.cu_new[s + 1], kv = b.kv_len[s];
-  SeqLen r = {a, e - a, kv, a >= 0 && e >= a && (uint32_t)e <= b.total_new, false};
+  SeqLen r = {a, e - a, kv, placed_ok(b, a, e), false};
   r.ok = r.placed && kv_len_ok(b, kv);
   if (!r.ok) report(b.status, GORGO_KV_BAD_LENGTH);
   return r;

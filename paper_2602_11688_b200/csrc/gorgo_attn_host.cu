@@ -102,7 +102,7 @@ KvView view(const gorgo_kv_cache_t* c) {
   return {c->k, c->v, c->k_exp, c->v_exp, c->n_pages, (uint32_t)__builtin_ctz(c->page_tokens), c->n_kv_heads};
 }
 BatchView view(const gorgo_kv_batch_t* b) {
-  return {b->cu_new, b->kv_len, b->table, b->status, b->n_seqs, b->total_new, b->max_kv, b->table_stride};
+  return {b->cu_new, b->kv_len, b->table, b->status, b->n_seqs, b->total_new, b->max_new, b->max_kv, b->table_stride};
 }
 
 int move(bool write, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, const void* k, const void* v, uint32_t type,

@@ -173,7 +173,7 @@ __device__ __forceinline__ uint32_t mma_shape(uint32_t n, bool bf16, bool negate
 // New rows of sequence s if its place in the packed array makes sense, else none.
 __device__ __forceinline__ int rows_of(const BatchView& b, uint32_t s) {
   const int a = b.cu_new[s], e = b.cu_new[s + 1];
-  if (a >= 0 && e >= a && (uint32_t)e <= b.total_new) return e - a;
+  if (placed_ok(b, a, e)) return e - a;
   report(b.status, GORGO_KV_BAD_LENGTH);
   return 0;
 }

@@ -98,3 +98,29 @@ def test_write_touches_nothing_for_rows_without_a_place():
         assert not bool((changed & ~allowed).any())
         pg, slot = m.where(0, torch.arange(27, 29 if fault == "decreasing" else 30, device="cuda"))   # (row 2 is two sequences' there)
         assert bool((m.cache.k[pg, :, slot] == 1).all())
+
+
+@pytest.mark.parametrize("call", ["write", "read", "prefill"])
+def test_more_new_tokens_than_max_new(call):
+    """The first sequence's rows, six of at most four, are reported and left; the others are served."""
+    from paper_2602_11688_b200 import binding as gb
+    m = Made(97, [3, 4, 2], [30, 70, 40], page=16)
+    m.batch.cu_new[1:3] = torch.tensor([6, 8], dtype=torch.int32)
+    want = [m.row(1, m.q[6 + i], 69 + i, 0.125) for i in range(2)] + [m.row(2, m.q[8], 40, 0.125)]
+    x = torch.zeros((9, 2, 64), dtype=BF16, device="cuda")
+    if call == "write":
+        before = m.cache.k.clone()
+        m.cache.write(m.batch, x, x)
+        for s, lo, hi, same in ((0, 24, 30, True), (1, 68, 70, False), (2, 39, 40, False)):
+            pg, slot = m.where(s, torch.arange(lo, hi, device="cuda"))
+            assert torch.equal(m.cache.k[pg, :, slot], before[pg, :, slot] if same else x[:hi - lo])
+    elif call == "read":
+        out = x + 7
+        m.cache.read(m.batch, out=(out, x))
+        assert bool((out[:6] == 7).all()) and torch.equal(out[6:], torch.cat([m.keys[1][-2:], m.keys[2][-1:]]).to(BF16))
+    else:
+        out = torch.full((9, 4, 64), 7.0, dtype=BF16, device="cuda")
+        m.cache.prefill(m.batch, m.q, out=out)
+        assert bool((out[:6] == 7).all())
+        check(out[6:], None, [torch.stack([w[i] for w in want]) for i in range(3)], BF16)
+    assert int(m.batch.status.item()) == gb.GORGO_KV_BAD_LENGTH
