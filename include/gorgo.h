@@ -493,11 +493,13 @@ const char *gorgo_strerror(int code);
  * holds a NaN or an infinity is stored in e4m3 as NaN throughout.
  *
  * The calls only enqueue kernels on `cuda_stream` (they may be captured into a graph) and keep nothing
- * between them.  All arrays are DEVICE memory of `device`.  The lengths and the table are read on the device: the
- * kernels check them, never leave the given arrays, and report what is wrong in `status` (bits
- * GORGO_KV_*, set and never cleared); outputs that need a wrong page (attention: the rows that see a token of it) and all
- * outputs of a sequence with a wrong length hold NaN (attention, read) or the wrong tokens are left out (write); rows of a
- * sequence whose place in the packed array makes no sense are left as they are.  A page that is written must not be in the table twice in one batch. */
+ * between them.  All arrays are DEVICE memory of `device`, aligned to their elements where nothing more is
+ * said.  The lengths and the table are read on the device: the kernels check them, never leave the given
+ * arrays, and report what is wrong in `status` (bits GORGO_KV_*, set and never cleared).  Outputs that need a
+ * wrong page (attention: the rows that see a token of it) and all outputs of a sequence with a wrong length
+ * hold NaN (attention, read) or the wrong tokens are left out (write); rows of a sequence whose place in the
+ * packed array makes no sense are left as they are.  A page that is written must not be in the table twice
+ * in one batch. */
 enum { GORGO_BF16 = 0, GORGO_FP16 = 1, GORGO_E4M3 = 2 };
 enum {
   GORGO_KV_BAD_PAGE = 1,              /* a table entry that is needed is outside [0, n_pages)       */

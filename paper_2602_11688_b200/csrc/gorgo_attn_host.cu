@@ -86,6 +86,7 @@ bool batch_ok(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, bool decode)
   if (b->n_seqs == 0) return true;
   if (b->total_kv >= 1ull << 40) return false;
   if (!b->kv_len || (!b->table && b->max_kv) || (!decode && !b->cu_new)) return false;
+  if (!aligned(b->kv_len, 4) || !aligned(b->table, 4) || !aligned(b->status, 4) || (!decode && !aligned(b->cu_new, 4))) return false;
   if (!decode && (b->total_new >= (1u << 24) || b->max_new > b->total_new)) return false;
   return b->max_kv < (1u << 24) && (uint64_t)b->table_stride * c->page_tokens >= b->max_kv;
 }
@@ -152,7 +153,7 @@ int attend(bool decode, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, co
   const uint64_t rows = b->n_seqs == 0 ? 0 : decode ? b->n_seqs : b->total_new;
   if (rows == 0) return GORGO_OK;
   const uint64_t width = (uint64_t)n_heads * c->head_dim;
-  if (rows * n_heads >= (1ull << 31) || !rows_ok(q, qs, width) || !rows_ok(out, os, width)) return GORGO_ERR_INVALID_ARG;
+  if (rows * n_heads >= (1ull << 31) || !rows_ok(q, qs, width) || !rows_ok(out, os, width) || !aligned(lse, 4)) return GORGO_ERR_INVALID_ARG;
   AttnArgs a = attn_args(c, b, n_heads, type);
   if (!decode && !prefill_fits(a)) return GORGO_ERR_INVALID_ARG;
   DeviceScope dev(c->device);

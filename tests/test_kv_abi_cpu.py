@@ -106,3 +106,20 @@ def test_null_structures_are_refused():
     assert set(calls(cache(), None).values()) == {gb.GORGO_ERR_INVALID_ARG}
     assert gb.load().gorgo_attn_workspace_bytes(C.addressof(cache()), C.addressof(batch()), 4, 0, 1, None) == \
         gb.GORGO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("what", ["kv_len", "table", "status", "cu_new"])
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_arrays_that_are_not_aligned_to_their_elements_are_refused(what, off):
+    got = calls(cache(), batch(**{what: A + off}))
+    assert got["write"] == got["read"] == got["prefill"] == gb.GORGO_ERR_INVALID_ARG
+    if what != "cu_new":
+        assert got["decode"] == gb.GORGO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_an_lse_that_is_not_aligned_is_refused(decode):
+    lib, c, b = gb.load(), cache(), batch()
+    f = lib.gorgo_attn_decode if decode else lib.gorgo_attn_prefill
+    assert f(C.addressof(c), C.addressof(b), A, 4, gb.GORGO_BF16, 256, 0.1, A, 256, A + 2, A, 4 << 30, None) == \
+        gb.GORGO_ERR_INVALID_ARG
