@@ -60,7 +60,7 @@ constexpr int kAhead = 2;
 template <typename T, bool kQuant, int D>
 __global__ void __launch_bounds__(kMoveThreads) kv_write_kernel(const KvMoveArgs a, const uint32_t n_tok) {
   constexpr uint32_t kLanes = D / 8, kRows = kMoveThreads / kLanes;
-  extern __shared__ int8_t gathered[];                         // [2][heads][n_tok], quantised only
+  extern __shared__ __align__(16) int8_t gathered[];           // [2][heads][n_tok], quantised only; read eight at a time
   __shared__ int64_t place[kMaxTok];
   const uint32_t first = blockIdx.x * n_tok;
   const uint32_t here = min(n_tok, a.b.total_new - first), hk = a.kv.n_kv_heads;
