@@ -432,13 +432,18 @@ int gorgo_measure_gather(int device, void *buffer, uint64_t buffer_bytes, uint64
  *   GORGO_DEBUG_BUILD       build of the replay kernel: 0 (default) chosen by the candidates of each
  *                           launch, 1 the one for at most a quarter as many candidates as the GPU has
  *                           SMs, 2 the one for up to two an SM, 3 the one for more (results do not
- *                           depend on it).  gorgo_replay_occupancy then reports that build. */
+ *                           depend on it).  gorgo_replay_occupancy then reports that build.
+ *   GORGO_DEBUG_KV_WAIT_TICKS  clock ticks after which a wait of gorgo_attn_prefill gives up, in
+ *                           every later call of the process (`sim` is not used and may be NULL); 2^32 - 1
+ *                           (default) is about ten seconds.  With 0 the first wait that is not
+ *                           already satisfied gives up: the status word says GORGO_KV_WAIT_LIMIT. */
 enum {
   GORGO_DEBUG_POLL_LIMIT = 0,
   GORGO_DEBUG_RING_POLLS = 1,
   GORGO_DEBUG_PROBE_OFF = 2,
   GORGO_DEBUG_SCOUT_OFF = 3,
-  GORGO_DEBUG_BUILD = 4
+  GORGO_DEBUG_BUILD = 4,
+  GORGO_DEBUG_KV_WAIT_TICKS = 5
 };
 int gorgo_debug_set(gorgo_sim_t *sim, uint32_t what, uint32_t value);
 
@@ -505,7 +510,8 @@ enum {
   GORGO_KV_BAD_PAGE = 1,              /* a table entry that is needed is outside [0, n_pages)       */
   GORGO_KV_BAD_LENGTH = 2,            /* cu_new or kv_len decreasing, negative or above its bound,  */
                                       /* more new tokens than max_new (all but decode)              */
-  GORGO_KV_WAIT_LIMIT = 4             /* a bounded wait inside a kernel ran out                     */
+  GORGO_KV_WAIT_LIMIT = 4             /* a bounded wait inside a kernel ran out: rows of the call's */
+                                      /* result may be NaN, or left as they were                    */
 };
 
 typedef struct gorgo_kv_cache {

@@ -43,7 +43,7 @@ EXPORTS = [
 GORGO_BF16, GORGO_FP16, GORGO_E4M3 = 0, 1, 2
 GORGO_KV_BAD_PAGE, GORGO_KV_BAD_LENGTH, GORGO_KV_WAIT_LIMIT = 1, 2, 4
 GORGO_DEBUG_POLL_LIMIT, GORGO_DEBUG_RING_POLLS, GORGO_DEBUG_PROBE_OFF, GORGO_DEBUG_SCOUT_OFF = 0, 1, 2, 3
-GORGO_DEBUG_BUILD = 4
+GORGO_DEBUG_BUILD, GORGO_DEBUG_KV_WAIT_TICKS = 4, 5
 
 
 class gorgo_config_t(C.Structure):

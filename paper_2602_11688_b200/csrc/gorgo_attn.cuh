@@ -57,7 +57,9 @@ struct AttnArgs {
   float scale_log2;                       // scale * log2(e)
   uint64_t total_kv;
   void* workspace;
+  long long wait_ticks;                   // clock ticks after which a wait gives up
 };
+void set_kv_wait_ticks(uint32_t ticks);   // 2^32 - 1: the default
 uint64_t decode_workspace(const AttnArgs& a, int sms);
 bool prefill_fits(const AttnArgs& a);           // whether the 16-bit copy of e4m3 pages has fewer than 2^31 rows
 uint64_t prefill_workspace(const AttnArgs& a, int sms);

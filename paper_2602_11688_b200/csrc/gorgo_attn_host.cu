@@ -52,6 +52,10 @@ bool make_rows_map(CUtensorMap* map, const void* q, uint32_t rows, uint32_t n_he
   return encode3(map, type, q, dims, strides, box);
 }
 
+// (a test switch of the process: nothing that a call depends on otherwise)
+static std::atomic<uint32_t> kv_wait_ticks{UINT32_MAX};
+void set_kv_wait_ticks(uint32_t ticks) { kv_wait_ticks.store(ticks, std::memory_order_relaxed); }
+
 }  // namespace gorgo
 
 namespace {
@@ -169,6 +173,8 @@ int attend(bool decode, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, co
   a.out_stride = os;
   a.scale_log2 = scale_log2;
   a.workspace = ws;
+  const uint32_t ticks = kv_wait_ticks.load(std::memory_order_relaxed);
+  a.wait_ticks = ticks == UINT32_MAX ? kWaitTicks : (long long)ticks;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   return (decode ? launch_attn_decode(a, sms, st) : launch_attn_prefill(a, sms, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
 }

@@ -1405,6 +1405,10 @@ int gorgo_measure_gather(int device, void* buffer, uint64_t buffer_bytes, uint64
 }
 
 int gorgo_debug_set(gorgo_sim_t* sim, uint32_t what, uint32_t value) {
+  if (what == GORGO_DEBUG_KV_WAIT_TICKS) {
+    gorgo::set_kv_wait_ticks(value);
+    return GORGO_OK;
+  }
   if (!sim) return GORGO_ERR_INVALID_ARG;
   switch (what) {
     case GORGO_DEBUG_POLL_LIMIT: sim->poll_limit = value; break;

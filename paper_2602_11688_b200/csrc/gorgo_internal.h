@@ -231,4 +231,6 @@ uint32_t mask_bytes_for(uint32_t n_replicas);
 // shared memory one CTA asks for.  `build` as in ReplayArgs; 0: the one for many candidates.
 int replay_occupancy(const Model& m, const TraceView& tr, uint32_t build, uint64_t* smem_bytes);
 
+void set_kv_wait_ticks(uint32_t ticks);   // test switch of the attention kernels (gorgo_attn_host.cu)
+
 }  // namespace gorgo

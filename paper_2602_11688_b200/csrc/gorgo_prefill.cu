@@ -69,7 +69,7 @@ struct Plan {
   float* part_ml;                         // [2 * grid][256][2]
   struct Split* split;                    // [grid]
   uint8_t* again;                         // [total_new][n_heads]: 1: the row's result is not finite and it has to be looked at
-  uint32_t* odd;                          // [grid]: whether a block has such rows
+  uint32_t* odd;                          // [grid]: 1: a block has such rows; 2: it gave up
 };
 
 struct Work {                             // a unit, or a block's part of it
@@ -350,13 +350,14 @@ struct Walk {
   __device__ uint32_t blocks_after() const { return (uint32_t)((unit_end * pieces - 1) / total) - blockIdx.x; }
 };
 
-// Waits; on the limit tells the block (and the host) to give up.
-__device__ __forceinline__ bool wait_or_give_up(uint32_t bar, uint32_t parity, volatile uint32_t* quit, uint32_t* status) {
+// Waits; on the limit tells the block (and the host) to give up.  Every role then leaves at its next wait, with what it has
+// started complete: copies landed, products done, entries of the ring of units as they were.
+__device__ __forceinline__ bool wait_or_give_up(uint32_t bar, uint32_t parity, long long limit, volatile uint32_t* quit, uint32_t* status) {
   if (mbar_try(bar, parity)) return true;
   const long long from = clock64();
   while (!mbar_try(bar, parity)) {
     if (*quit) return false;
-    if (clock64() - from > kWaitTicks) {
+    if (clock64() - from > limit) {
       *quit = 1;
       report(status, GORGO_KV_WAIT_LIMIT);
       return false;
@@ -447,7 +448,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   __syncthreads();
   fence_after();
   const uint32_t tmem = tmem_base;
-  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_or_give_up(bar, parity, &quit, a.b.status); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_or_give_up(bar, parity, a.wait_ticks, &quit, a.b.status); };
   auto steps_of = [](const Work& w, int i) { return max(0, min(w.hi, w.tiles[i]) - w.lo); };
 
   // Registers: 384 threads of 168 at the launch; the softmax takes what the last warpgroup does not need
@@ -606,7 +607,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         }
         if (mine && a.lse) a.lse[row * a.n_heads + head] = bad ? NAN : l == 0.f ? -INFINITY : (m * c - kShift<M> + log2f(l)) * 0.693147180559945309f;
         // (a sum that is not finite: the scores are the cause)
-        odd = mine && odd && l < INFINITY;
+        odd = mine && odd && !bad && l < INFINITY;
         if (mine) p.again[row * a.n_heads + head] = odd;
         if (odd) any_odd = 1;
       }
@@ -676,11 +677,10 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         __syncwarp();
         if (lane == 0) mbar_arrive(work_empty + 8 * e);
       }
-      if (quit) {                         // what flies has to land before the block ends
-        mbar_wait(q_full, q_phase);
-        for (uint32_t i = 0; i < min(copied, (uint32_t)Z::kSlots); ++i)
-          mbar_wait(full + 8 * i, i < slot ? phase ^ 1 : phase);         // the last copy into the slot
-      }
+      // what flies has to land before the block ends, whichever role gives up, and when
+      mbar_wait(q_full, q_phase);
+      for (uint32_t i = 0; i < min(copied, (uint32_t)Z::kSlots); ++i)
+        mbar_wait(full + 8 * i, i < slot ? phase ^ 1 : phase);           // the last copy into the slot
     } else if (warp == 9) {
       // -------------------------------------------------------------- products: one thread, nothing between two waits
       // but the issue itself (the tensor pipe takes few instructions ahead, so what this thread does besides shows)
@@ -738,7 +738,8 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
               clear_slot = v_slot;
               clear_from = behind;
               mbar_arrive(clear);
-              if (!(go = wait(cleared, c_phase))) break;
+              if (!(go = mbar_wait(cleared, c_phase))) break;  // (always answered, so never left: the next request would
+                                                               // take `clear` past the phase that warp 11 waits for)
               c_phase ^= 1;
             }
             const uint32_t k_slot = slot;
@@ -767,10 +768,8 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
             if (j + 2 == most) mma_commit(q_empty);
           }
         }
-        if (quit) {                       // products in flight end before the block does
-          mma_commit(drained);
-          mbar_wait(drained, 0);
-        }
+        mma_commit(drained);              // products in flight end before the block does
+        mbar_wait(drained, 0);
         clear_slot = kWhole;              // (ends warp 11)
         mbar_arrive(clear);
       }
@@ -785,6 +784,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
       for (uint32_t e = 0, e_phase = 1; go; e = (e + 1) % kEntries, e_phase ^= e == 0) {
         more = more && walk.next(a, p, step, w);
         go = __all_sync(0xffffffffu, wait(work_empty + 8 * e, e_phase));
+        if (!go) break;                   // (the entry is still read)
         if (lane == 0) {
           if (more) {
             ring[e] = w;
@@ -808,9 +808,9 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
         // (the products' thread always comes to an end and says so; this wait may last as long as all of the work)
         const long long began = clock64();
         bool asked;
-        while (!(asked = mbar_try(clear, c_phase)) && clock64() - began < 64 * kWaitTicks) {}
+        while (!(asked = mbar_try(clear, c_phase)) && clock64() - began < 64 * kWaitTicks) {}   // (not the limit a test sets)
         if (!__all_sync(0xffffffffu, asked)) break;
-        const uint32_t slot = clear_slot, from = clear_from;
+        const uint32_t slot = __shfl_sync(0xffffffffu, clear_slot, 0), from = __shfl_sync(0xffffffffu, clear_from, 0);
         if (slot == kWhole) break;
         const uint32_t rest = (kKeys - from) * 8;              // 16-byte pieces of a plane
         for (uint32_t x = lane; x < rest * Z::kPlanes; x += 32)
@@ -824,7 +824,7 @@ prefill_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Plan 
   __syncthreads();
   fence_after();
   if (warp == 9) tmem_free(tmem, 512);
-  if (threadIdx.x == 0) p.odd[blockIdx.x] = any_odd;
+  if (threadIdx.x == 0) p.odd[blockIdx.x] = any_odd | (quit ? 2 : 0);
 }
 
 // Keys that the tile of rows of a sequence's new token t took.
@@ -868,7 +868,7 @@ prefill_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
   if (blockIdx.y < kListBlocks) {
     uint32_t odd_rows = 0;
     for (uint32_t x = lane; x < gridDim.x; x += 32) odd_rows |= p.odd[x];
-    if (__any_sync(0xffffffffu, odd_rows != 0)) mend_list<T, D>(a, p, lane);
+    if (__any_sync(0xffffffffu, odd_rows & 1)) mend_list<T, D>(a, p, lane);
   }
   const Work w = p.split[c0].w;           // (read beside `parts`, whatever that says)
   const uint32_t parts = p.split[c0].parts;
@@ -888,6 +888,7 @@ prefill_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     float o[kPer];
 #pragma unroll
     for (int y = 0; y < kPer; ++y) o[y] = p.part_o[at(k) * D + lane * kPer + y];
+    if (p.odd[c0 + k] & 2) sum = NAN;     // (its part may not be there)
     if (ml.y == 0.f) continue;            // (it has no O: what was read is nothing)
     const float now = fmaxf(top, ml.x);
     const float f = top == now ? 1.f : fast_exp2(top - now), g = ml.x == now ? 1.f : fast_exp2(ml.x - now);

@@ -17,6 +17,10 @@ bool make_pool_map(CUtensorMap* map, const void* pool, uint64_t rows, uint32_t h
 bool make_rows_map(CUtensorMap* map, const void* q, uint32_t rows, uint32_t n_heads, uint32_t head_dim, uint64_t stride,
                    uint32_t type, uint32_t box_rows, uint32_t box_heads);
 
+// Clock ticks after which a wait gives up: about ten seconds, many times what a unit of work takes (2^24 keys in prefill:
+// 131,072 steps of 3,300 ticks, 0.25 s).
+constexpr long long kWaitTicks = 20000000000ll;
+
 #ifdef __CUDACC__
 
 // Lets a kernel have `bytes` of shared memory on the current device (once: the setting stays).
@@ -52,9 +56,6 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// Clock ticks after which a wait gives up: about ten seconds, many times what a unit of work takes (2^24 keys in prefill:
-// 131,072 steps of 3,300 ticks, 0.25 s).
-constexpr long long kWaitTicks = 20000000000ll;
 static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
   const long long from = clock64();
   while (!mbar_try(bar, parity))
