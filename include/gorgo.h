@@ -433,10 +433,10 @@ int gorgo_measure_gather(int device, void *buffer, uint64_t buffer_bytes, uint64
  *                           launch, 1 the one for at most a quarter as many candidates as the GPU has
  *                           SMs, 2 the one for up to two an SM, 3 the one for more (results do not
  *                           depend on it).  gorgo_replay_occupancy then reports that build.
- *   GORGO_DEBUG_KV_WAIT_TICKS  clock ticks after which a wait of gorgo_attn_prefill gives up, in
- *                           every later call of the process (`sim` is not used and may be NULL); 2^32 - 1
- *                           (default) is about ten seconds.  With 0 the first wait that is not
- *                           already satisfied gives up: the status word says GORGO_KV_WAIT_LIMIT. */
+ *   GORGO_DEBUG_KV_WAIT_TICKS  clock ticks after which a wait of gorgo_attn_prefill or
+ *                           gorgo_attn_decode gives up, in every later call of the process (`sim` is not used and may be NULL); 2^32 - 1
+ *                           (default) is about ten seconds.  With 0 a wait gives up that is not
+ *                           satisfied at a second look: the status word says GORGO_KV_WAIT_LIMIT. */
 enum {
   GORGO_DEBUG_POLL_LIMIT = 0,
   GORGO_DEBUG_RING_POLLS = 1,

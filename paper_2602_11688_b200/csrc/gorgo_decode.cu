@@ -126,6 +126,15 @@ __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, ui
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Waits for the copies into the `flying` stages from `st` on.
+__device__ __noinline__ void land(uint32_t bars, uint32_t stages, uint32_t st, uint32_t phase, uint32_t flying) {
+  for (; flying; --flying) {
+    mbar_wait(bars + 8 * st, phase);
+    if (++st == stages) { st = 0; phase ^= 1; }
+  }
+  __syncwarp();
+}
+
 // Byte offset of 16-byte chunk c of row r inside a slice, as the bulk copy's swizzle lays it out.
 template <bool kQuant, int D>
 __device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) {
@@ -307,9 +316,11 @@ decode_kernel(const AttnArgs a, const Split sp, const __grid_constant__ CUtensor
 
     const int n_keys = use.kv - (int)(use.tile * Z::kTile + warp * kSlice);
     const uint32_t bar = bar_a + 8 * st;
-    if (flying && !__all_sync(0xffffffffu, mbar_wait(bar, phase))) {
-      alive = false;                      // no more copies; those that fly are waited for in their turn
+    if (flying && !__all_sync(0xffffffffu, mbar_wait(bar, phase, a.wait_ticks))) {
+      alive = false;                      // no more copies; those that fly land before the block ends
       if (lane == 0) report(a.b.status, GORGO_KV_WAIT_LIMIT);
+      land(bar_a, Z::kStages, st, phase, flying);
+      flying = 0;
     }
     if (n_keys > 0 && alive) {
       bad |= bad_page[st] != 0;

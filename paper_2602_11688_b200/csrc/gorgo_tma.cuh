@@ -56,14 +56,25 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+// (without the pause that a try takes)
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, long long limit) {
+  if (limit == 0) return mbar_test(bar, parity);
   const long long from = clock64();
   while (!mbar_try(bar, parity))
-    if (clock64() - from > kWaitTicks) return false;
+    if (clock64() - from > limit) return false;
   return true;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-  return mbar_try(bar, parity) || mbar_wait_slow(bar, parity);
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long long limit = kWaitTicks) {
+  return mbar_try(bar, parity) || mbar_wait_slow(bar, parity, limit);
 }
 
 // rows [row, row + box) of the pool, all planes, to shared memory

@@ -49,3 +49,31 @@ def test_prefill_gives_up(limit, dtype, store, new, kv, heads, kv_heads, dim):
         m.batch.check()
     if n > 1000:
         assert said[0] == gb.GORGO_KV_WAIT_LIMIT
+
+
+@pytest.mark.parametrize("dtype,store", [(BF16, BF16), (FP16, FP16), (BF16, E4M3), (FP16, E4M3)])
+@pytest.mark.parametrize("kv,heads,kv_heads,dim", [((1,), 4, 2, 64), ((30000, 0, 300, 60000), 16, 8, 128), ((70,) * 200, 16, 1, 64)])
+def test_decode_gives_up(limit, dtype, store, kv, heads, kv_heads, dim):
+    from paper_2602_11688_b200 import binding as gb
+    m = Made(131, [1] * len(kv), kv, heads=heads, kv_heads=kv_heads, dim=dim, dtype=dtype, store=store, page=64)
+    n = len(kv)
+    first = m.cache.decode(m.batch, m.q)
+    m.batch.check()
+    said = []
+    for ticks in (0, 300, 1000, 2000, 4000, 16000):
+        limit(ticks)
+        out = torch.empty((n + 2, heads, dim), dtype=dtype, device="cuda")
+        for _ in range(5):
+            out.fill_(7.0)
+            m.cache.decode(m.batch, m.q, out=out)
+            same = (out[:n].view(torch.int16) == first.view(torch.int16)).all(-1)
+            assert bool((same | torch.isnan(out[:n]).all(-1)).all())
+            assert bool((out[n:] == 7).all())
+            said.append(int(m.batch.status.item()))
+            assert said[-1] == (0 if bool(same.all()) else gb.GORGO_KV_WAIT_LIMIT)
+            m.batch.status.zero_()
+        limit((1 << 32) - 1)
+        assert torch.equal(m.cache.decode(m.batch, m.q).view(torch.int16), first.view(torch.int16))
+        m.batch.check()
+    if max(kv) > 1000 and store != E4M3:                     # more than the L2 holds; codes may arrive before they are waited for
+        assert gb.GORGO_KV_WAIT_LIMIT in said[:5]
