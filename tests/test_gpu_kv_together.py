@@ -103,3 +103,19 @@ def test_the_tuner_measures_its_service_model(kv_type, capsys):
     assert len(s["prefill"]) > 0 and [b for b, _ in s["decode"]] == [1, 2, 4]
     table = lines[-1]["p95_ttft_ms_and_p95_e2e_ms"]
     assert "gorgo-tuned" in table and all(np.isfinite(v).all() and min(v) > 0 for v in table.values())
+
+
+def test_the_measured_times_are_the_gpus(monkeypatch):
+    """A host that takes its time between a layer's calls changes nothing: an engine replays a graph."""
+    import time
+    from paper_2602_11688_b200 import service as S
+    from paper_2602_11688_b200 import workloads as W
+    rest = S.EngineLayer._rest
+
+    def slow(self, x, attended):
+        time.sleep(0.01)
+        return rest(self, x, attended)
+
+    monkeypatch.setattr(S.EngineLayer, "_rest", slow)
+    s = S.measure(W.make_workload("tiny", population=1, n_requests=300), S.EngineShape(1, 256, 512, 8, 2, 64), samples=2)
+    assert all(t < 5.0 for _, t in s["decode"]) and all(t < 5.0 for *_, t in s["prefill"])
