@@ -134,18 +134,28 @@ def fit_decode(busy, ms):
     return at0, slope / at0
 
 
+def cache_and_budget(blocks: int, w):
+    """(blocks of the prefix cache, tokens of requests that run) where there is memory for ``blocks`` blocks: prompts
+    of running requests lie in the cache's blocks; their answers, up to the workload's longest in every slot,
+    take the others."""
+    answers = w.spec.slots * -(-int(w.output_tokens.max()) // w.spec.block_tokens)
+    if blocks <= answers:
+        raise ValueError("the weights leave no room for a cache block beside the running requests' answers")
+    return blocks - answers, (blocks - answers) * w.spec.block_tokens
+
+
 def measure(w, shape: EngineShape, kv_type: str = "bf16", *, device: int = 0, samples: int = 16, repeats: int = 5,
             memory_share: float = 0.9, seed: int = 0):
     """The service model's constants for workload ``w`` on an engine of ``shape``: a dict of
     ``prefill_ms_per_token``, ``tpot_ms``, ``decode_slowdown``, ``cache_blocks``, ``kv_budget_tokens`` and what
-    they were fitted to.  The cache has what ``memory_share`` of the GPU's memory leaves beside the weights."""
+    they were fitted to.  The cache has what ``memory_share`` of the GPU's memory leaves beside the weights and the
+    running requests' answers."""
     import torch
     from . import binding as gb
     block = w.spec.block_tokens
     blocks = int((torch.cuda.get_device_properties(device).total_memory * memory_share - shape.weight_bytes())
                  // shape.block_bytes(block, kv_type))
-    if blocks < 1:
-        raise ValueError("the weights leave no room for a cache block")
+    blocks, budget = cache_and_budget(blocks, w)
     drawn = requests_of(w, max(samples, w.spec.slots), seed)
     if not drawn:
         raise ValueError("the workload has no request with uncached tokens")
@@ -197,4 +207,4 @@ def measure(w, shape: EngineShape, kv_type: str = "bf16", *, device: int = 0, sa
     tpot, slowdown = fit_decode(*zip(*decode))
     return {"prefill_ms_per_token": fit_prefill([u for u, _, _ in prefill], [t for _, _, t in prefill]),
             "tpot_ms": tpot, "decode_slowdown": slowdown, "cache_blocks": blocks,
-            "kv_budget_tokens": blocks * block, "prefill": prefill, "decode": decode}
+            "kv_budget_tokens": budget, "prefill": prefill, "decode": decode}

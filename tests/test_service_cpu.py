@@ -36,3 +36,15 @@ def test_requests_are_what_the_previous_turn_leaves_uncached():
     got = sorted(S.requests_of(w, 10))
     assert got == sorted([(1000, 1000), (1600 - 512, 1600), (700, 700), (2000 - 3 * 512, 2000)])
     assert len(S.requests_of(w, 2)) == 2
+
+
+def test_memory_is_given_once():
+    """What the prefix cache holds and what the running requests' answers take is the memory that there is."""
+    reqs = [(0.0, 1000, 600, [1, 2]), (1.0, 1600, 1030, [1, 3, 4, 5])]
+    w = W.handmade(np.array([5.0, 6.0]), reqs, slots=3, cache_blocks=50, params=np.ones((1, 3)))
+    blocks, tokens = S.cache_and_budget(100, w)
+    assert blocks == 100 - 3 * 3                             # three slots, answers of up to 1,030 tokens
+    assert tokens == blocks * 512                            # prompts of running requests lie in the cache's blocks
+    assert S.cache_and_budget(10, w) == (1, 512)
+    with pytest.raises(ValueError):
+        S.cache_and_budget(9, w)
