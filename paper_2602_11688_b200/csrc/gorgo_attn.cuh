@@ -40,6 +40,7 @@ struct KvMoveArgs {
   void* v_out;
   uint64_t k_stride, v_stride;            // elements from token to token
   uint32_t head_dim, type, store;
+  uint32_t sms;                           // of the device
   uint64_t per_head;                      // set by the launcher: a division as a product
 };
 cudaError_t launch_kv_write(const KvMoveArgs& a, cudaStream_t st);

@@ -110,23 +110,6 @@ BatchView view(const gorgo_kv_batch_t* b) {
   return {b->cu_new, b->kv_len, b->table, b->status, b->n_seqs, b->total_new, b->max_new, b->max_kv, b->table_stride};
 }
 
-int move(bool write, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, const void* k, const void* v, uint32_t type,
-         uint64_t ks, uint64_t vs, void* stream) {
-  if (!cache_ok(c) || !batch_ok(c, b, false) || !type_ok(c, type)) return GORGO_ERR_INVALID_ARG;
-  if (b->n_seqs == 0 || b->total_new == 0) return GORGO_OK;
-  const uint64_t width = (uint64_t)c->n_kv_heads * c->head_dim;
-  if (!rows_ok(k, ks, width) || !rows_ok(v, vs, width)) return GORGO_ERR_INVALID_ARG;
-  DeviceScope dev(c->device);
-  if (!dev.ok) return GORGO_ERR_CUDA;
-  KvMoveArgs a = {view(c), view(b), k, v, const_cast<void*>(k), const_cast<void*>(v), ks, vs, c->head_dim, type, c->type};
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return (write ? launch_kv_write(a, st) : launch_kv_read(a, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
-}
-
-bool heads_ok(const gorgo_kv_cache_t* c, uint32_t n_heads) {
-  return n_heads && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= 128;
-}
-
 int sm_count(int device) {
   static std::atomic<int> known[64];
   int n = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
@@ -134,6 +117,24 @@ int sm_count(int device) {
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
   if (device < 64) known[device].store(n, std::memory_order_relaxed);
   return n;
+}
+
+int move(bool write, const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, const void* k, const void* v, uint32_t type,
+         uint64_t ks, uint64_t vs, void* stream) {
+  if (!cache_ok(c) || !batch_ok(c, b, false) || !type_ok(c, type)) return GORGO_ERR_INVALID_ARG;
+  if (b->n_seqs == 0 || b->total_new == 0) return GORGO_OK;
+  const uint64_t width = (uint64_t)c->n_kv_heads * c->head_dim;
+  if (!rows_ok(k, ks, width) || !rows_ok(v, vs, width)) return GORGO_ERR_INVALID_ARG;
+  DeviceScope dev(c->device);
+  const int sms = dev.ok ? sm_count(c->device) : 0;
+  if (!sms) return GORGO_ERR_CUDA;
+  KvMoveArgs a = {view(c), view(b), k, v, const_cast<void*>(k), const_cast<void*>(v), ks, vs, c->head_dim, type, c->type, (uint32_t)sms};
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return (write ? launch_kv_write(a, st) : launch_kv_read(a, st)) == cudaSuccess ? GORGO_OK : GORGO_ERR_CUDA;
+}
+
+bool heads_ok(const gorgo_kv_cache_t* c, uint32_t n_heads) {
+  return n_heads && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= 128;
 }
 
 AttnArgs attn_args(const gorgo_kv_cache_t* c, const gorgo_kv_batch_t* b, uint32_t n_heads, uint32_t type) {

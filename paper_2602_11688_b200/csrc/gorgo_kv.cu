@@ -205,8 +205,8 @@ cudaError_t launch_move(const KvMoveArgs& a, cudaStream_t st) {
   // 4.9; 400 written in e4m3 the other way round 4.6 and 3.7, 1,000 again 4.7 and 5.8).  Many: eight, or 32 where codes are written (128,000 tokens:
   // 154 against 165 us; read, 32 are 360 against 349 us), if the gathered powers of two leave room for them.
   const bool codes = kWrite && kQuant;
-  const uint32_t n_tok = a.b.total_new < (codes ? 4u : 2u) * 148u ? 1
-                         : a.b.total_new < 8u * 148u * 32u || !codes || a.kv.n_kv_heads > 64 ? 8 : kMaxTok;
+  const uint32_t n_tok = a.b.total_new < (codes ? 4u : 2u) * a.sms ? 1
+                         : a.b.total_new < 8u * a.sms * 32u || !codes || a.kv.n_kv_heads > 64 ? 8 : kMaxTok;
   const uint32_t grid = (a.b.total_new + n_tok - 1) / n_tok;
   if (kWrite) kv_write_kernel<T, kQuant, D><<<grid, kMoveThreads, kQuant ? 2 * a.kv.n_kv_heads * n_tok : 0, st>>>(a, n_tok);
   else kv_read_kernel<T, kQuant, D><<<grid, kMoveThreads, 0, st>>>(a, n_tok);
