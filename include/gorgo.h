@@ -559,14 +559,15 @@ int gorgo_kv_read(const gorgo_kv_cache_t *cache, const gorgo_kv_batch_t *batch, 
                   void *cuda_stream);
 
 /* Attention of queries against the pages.  q, out: DEVICE rows of `type` (bf16 or fp16; the cache's own
- * unless that is e4m3), n_heads a multiple of n_kv_heads (at most 128 times as many), query head h reads kv head
- * h / (n_heads / n_kv_heads); row strides in elements, multiples of 8, 16-byte aligned; out does not overlap
- * q.  With z_j = scale * (q . k_j)
- * over the keys j that a row sees: out = sum_j exp(z_j) v_j / sum_j exp(z_j), lse (DEVICE
- * float [rows][n_heads], or NULL) = log sum_j exp(z_j).  A row that sees no key, or none whose
- * score is above -inf, gets zeros and -inf.  What a row does not see does not reach it, whatever it holds; a value it sees
- * that is not finite makes that element of its result not finite (NaN or infinite), a score that is NaN or +inf (in 32 bits,
- * times log2(e)) the whole row.  GORGO_ERR_NONFINITE_PARAM: `scale` is not finite in 32 bits.
+ * unless that is e4m3), n_heads a multiple of n_kv_heads (at most 128 times as many), query head h reads
+ * kv head h / (n_heads / n_kv_heads); row strides in elements, multiples of 8, 16-byte aligned; out does
+ * not overlap q.  With z_j = scale * (q . k_j) over the keys j that a row sees:
+ * out = sum_j exp(z_j) v_j / sum_j exp(z_j), lse (DEVICE float [rows][n_heads], or NULL) = log sum_j exp(z_j).
+ * A row that sees no key, or none whose score is above -inf, gets zeros and -inf.  What a row does not see
+ * does not reach it, whatever it holds; a value it sees that is not finite makes that element of its result
+ * not finite (NaN or infinite), a score that is NaN or +inf (in 32 bits, times log2(e)) the whole row.  Sums
+ * are held in 32 bits: elements of values beyond 2^100 may come out infinite.  GORGO_ERR_NONFINITE_PARAM:
+ * `scale` is not finite in 32 bits.
  *   gorgo_attn_prefill: one row per new token; the token at position p of its sequence sees the keys 0..p
  * (those of the new tokens are written first).  Rows behind cu_new[n_seqs] are left as they are.
  *   gorgo_attn_decode: one row per sequence, which sees all its kv_len[s] keys; cu_new, total_new and

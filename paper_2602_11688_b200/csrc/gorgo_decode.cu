@@ -21,8 +21,8 @@
 // of P.  Those powers may be 2^144 apart, so for l the exponentials are taken 2^30 larger, and a factor between maxima is applied
 // to l as two square roots: neither loses a key that counts.
 //
-// Measured (32 query heads, 8 kv heads, head dim 128): 16 sequences of about 20,000 tokens in bf16, 1.47 GB, 227 us: 6.5 TB/s;
-// 64 in e4m3, 3.6 GB, 640 us: 5.7 TB/s; four of about 1,000: 12.4 us in a graph, latency.
+// Measured (32 query heads, 8 kv heads, head dim 128): 16 sequences of about 20,000 tokens in bf16, 1.47 GB, 228 us: 6.4 TB/s;
+// 64 in e4m3, 3.6 GB, 646 us: 5.6 TB/s (with pauses 579); four of about 1,000: 12.4 us in a graph, latency.
 #include "gorgo_tma.cuh"
 
 namespace gorgo {

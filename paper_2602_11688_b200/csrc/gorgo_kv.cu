@@ -4,8 +4,9 @@
 // (2 + stored bytes) bytes for T tokens, and for a handful of tokens the launch and the chain
 // cu_new -> table -> row.  A block takes a few tokens with all their heads: one warp finds the sequences, pages and slots
 // while the rows are already being loaded; 16 bytes a lane.
-// Measured, of 6,538 GB/s that a copy reaches: new turns in bf16 (273 MB) 47.9 us, 5.7 TB/s; 128,000 tokens written in e4m3
-// (789 MB) 154 us, 5.1 TB/s, bound by its instructions; e4m3 prefixes read in bf16 (2.2 GB) 349 us, 6.3 TB/s.
+// Measured, of 6,538 GB/s that a copy reaches: new turns in bf16 (273 MB) 47.7 us, 5.7 TB/s; 128,000 tokens written in e4m3
+// (789 MB) 161 us back to back, 4.9 TB/s (with pauses 154), bound by its instructions; e4m3 prefixes read in bf16 (2.2 GB)
+// 356 us, 6.2 TB/s.
 #include "gorgo_attn.cuh"
 
 namespace gorgo {

@@ -19,7 +19,8 @@
 // Values behind the last key of a sequence may be anything: they are overwritten with zeros in shared memory.  A value
 // that is not finite and that a row of its tile does not see would reach the row as 0 * x: rows whose result is not
 // finite are listed (a byte a row and head), and the second kernel, in which nothing waits for another warp, looks at the
-// values behind their own last key and computes them again key by key if one of those is the cause (one row of 100,000 keys: 34 ms; 18,900 rows of 30,000: 108 ms).
+// values behind their own last key and computes them again key by key if one of those is the cause (one row of
+// 100,000 keys: 34 ms; 18,900 rows of 30,000: 108 ms).
 //
 // All (sequence, kv head, tokens) units with their tiles of keys, and two places more for what a unit costs besides, are
 // laid out as one line that is cut into as many equal pieces as SMs: no batch, no lengths and no long prefix under a few
@@ -30,9 +31,13 @@
 // them: what a code stands for need not fit fp16, and q need not fit bf16; so q is taken as the sum of two bf16 numbers
 // (exactly) and P, too, is held as two: twice the products, 16 bits of P.
 //
-// Measured (32 query heads, 8 kv heads, head dim 128, bf16): 20,000 tokens 2.50 ms, 1,311 TFLOP/s of 1,679 that the library's
-// products reach at burst clocks (back to back, under the power cap, 2.93 ms); sixteen prompts of about 1,000 tokens 410 us,
-// 896 TFLOP/s; two turns of 1,000 on 20,000 1.40 ms, 1,103 TFLOP/s, in e4m3 1.46 ms.  Head dim 64: 737 TFLOP/s.
+// P is rounded to 16 bits once, and l sums it before that: the result is off by 2.1e-3 in bf16 (2-norm) where its own
+// rounding makes 1.6e-3; to hold P as two numbers always would cost half again as many products.
+//
+// Measured (32 query heads, 8 kv heads, head dim 128, bf16), passes with pauses and, in brackets, back to back under the power
+// cap: 20,000 tokens 2.57 (2.97) ms, 1,277 (1,105) TFLOP/s of 1,679 (1,389) that the library's products reach; sixteen prompts
+// of about 1,000 tokens 416 (472) us, 882 (778); two turns of 1,000 on 20,000 1.45 ms, 1,066, in e4m3 1.54 (1.79) ms, with fp16
+// queries 2.30 ms.  Head dim 64, 20,000 tokens: 2.3 to 2.6 ms, 630 to 710 TFLOP/s.
 #include "gorgo_rows.cuh"
 #include "gorgo_tma.cuh"
 
